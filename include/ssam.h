@@ -424,6 +424,41 @@ int ssam_neck(const void *x, const void *w1, const float *ln1_g, const float *ln
               int B, int g, int D, int C, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* Gradients: what a training step of the block needs beside the calls above  */
+/* ------------------------------------------------------------------------- */
+
+/* Gradient of ssam_ln_gather.  With h = (x - mean) * rstd of the row that output row p was made from, g = dy * gamma:
+ *   dx row  (+)= rstd * (g - mean_D(g) - h * mean_D(g * h)),  dgamma = sum dy * h,  dbeta = sum dy  (sums over all rows).
+ * x, idx, idx_batch_stride, gamma, eps, B, Nin, Nout, D as in the forward call; dy dev bf16 [B][Nout][D].
+ * dx dev bf16 [B][Nin][D]: row idx[b][p] of image b is written, or with accumulate != 0 added to (one rounding of the
+ * sum): the gradient of a residual stream, updated in place.  Rows that idx does not name, and with idx outside
+ * [0,Nin) none, are left untouched.  idx must not name a row of an image twice.  dx must not overlap x or dy.
+ * dgamma, dbeta dev fp32 [D], written; both NULL: not wanted (then the workspace may be NULL too).  Rows with
+ * idx < 0 add nothing to them.  Statistics are taken again from x; all sums are fp32, in a fixed order.
+ * D <= 2048 and B*Nout below 2^31 - 65536, else SSAM_EUNSUPPORTED. */
+size_t ssam_ln_gather_backward_workspace_bytes(int B, int Nout, int D);
+int ssam_ln_gather_backward(const void *x, const int32_t *idx, int idx_batch_stride, const float *gamma, float eps,
+                            const void *dy, void *dx, int accumulate, float *dgamma, float *dbeta,
+                            int B, int Nin, int Nout, int D, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Activations kept in 8 bits from the forward to the backward pass.  Of every row, 64 columns in turn (the last ones
+ * fewer where D is no multiple) share a scale: scales[row][j] = max|x| / 127, codes[row][c] = rint(x * 127 / max|x|),
+ * ties to even, in -127..127; the value held is codes * scale, off by at most max|x| / 254.  Scales below 2^-126 become
+ * 2^-126 (off by 2^-127 at most).  Infinity or NaN in a block makes its scale NaN, and all of its values with it.
+ * codes dev int8 [rows][D], scales dev fp32 [rows][ceil(D/64)].  D % 8 == 0, D <= 2^24 (else SSAM_EUNSUPPORTED).
+ *   ssam_checkpoint_store:   x dev bf16 [rows][D] -> codes, scales
+ *   ssam_checkpoint_restore: codes, scales -> x = bf16(codes * scale)
+ *   ssam_gelu_checkpoint:    h dev bf16 [rows][D] -> a = bf16(gelu_erf(h)), and codes and scales of h: the routed MLP's
+ *                            activation between fc1 (SSAM_EPI_BIAS) and fc2.  a may be h.
+ *   ssam_gelu_backward:      with t = codes * scale (fp32): dh = bf16(da * gelu'(t)), and, unless a is NULL,
+ *                            a = bf16(gelu_erf(t)), which the gradient of fc2's weight is formed with.  da, dh, a dev
+ *                            bf16 [rows][D].  dh may be da. */
+int ssam_checkpoint_store(const void *x, void *codes, float *scales, long rows, int D, void *stream);
+int ssam_checkpoint_restore(const void *codes, const float *scales, void *x, long rows, int D, void *stream);
+int ssam_gelu_checkpoint(const void *h, void *a, void *codes, float *scales, long rows, int D, void *stream);
+int ssam_gelu_backward(const void *codes, const float *scales, const void *da, void *dh, void *a, long rows, int D, void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* Instrumentation for the benchmark's measured peaks (not part of the method) */
 /* ------------------------------------------------------------------------- */
 

@@ -54,7 +54,8 @@ def lib():
         L.ssam_status_string.restype = C.c_char_p
         for n in ("ssam_score_tokens_workspace_bytes", "ssam_routed_mlp_workspace_bytes",
                   "ssam_encoder_block_workspace_bytes", "ssam_encoder_workspace_bytes", "ssam_linear_workspace_bytes",
-                  "ssam_patch_embed_workspace_bytes", "ssam_neck_workspace_bytes"):
+                  "ssam_patch_embed_workspace_bytes", "ssam_neck_workspace_bytes",
+                  "ssam_ln_gather_backward_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         L.ssam_probe_mfma_flops.restype = C.c_double
         _lib = L
@@ -537,6 +538,115 @@ def ssam_neck(x, w1, ln1_g, ln1_b, w2, ln2_g, ln2_b, g, eps=1e-6, out=None, work
         _f32(ln2_b, "ln2_b"), C.c_float(eps), _bf(out, "out"), C.c_int(Bn), C.c_int(g), C.c_int(D), C.c_int(Cn),
         C.c_void_p(workspace.data_ptr()), C.c_size_t(workspace.numel()), _stream()))
     return out
+
+
+# ------------------------------------------------------------------ gradients
+def _one_device(**tensors):
+    """Kernels run on the current device: a tensor that lies on another one is refused."""
+    here = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.device.index != here:
+            raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{here}")
+
+
+def _shape(t, want, name):
+    if t is not None and tuple(t.shape) != tuple(want):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(want)}")
+
+
+def ssam_ln_gather_backward_workspace_bytes(B, Nout, D) -> int:
+    return lib().ssam_ln_gather_backward_workspace_bytes(C.c_int(B), C.c_int(Nout), C.c_int(D))
+
+
+def ssam_ln_gather_backward(x, idx, idx_batch_stride, gamma, eps, dy, dx=None, accumulate=False, weight_grads=True, workspace=None):
+    """x [B,Nin,D], dy [B,Nout,D] bf16; idx int32 as given to ssam_ln_gather -> (dx [B,Nin,D] bf16, dgamma [D], dbeta [D] fp32).
+    dx: updated in place (accumulate: added to); None: a new one, zero where idx names no row."""
+    B, Nin, D = x.shape
+    Nout = dy.shape[1]
+    ptrs = [_bf(x, "x"), _i32(idx, "idx"), C.c_int(idx_batch_stride), _f32(gamma, "gamma"), C.c_float(eps), _bf(dy, "dy")]
+    _shape(dy, (B, Nout, D), "dy")
+    _shape(gamma, (D,), "gamma")
+    if idx.numel() < (B - 1) * idx_batch_stride + Nout:
+        raise ValueError(f"idx: {idx.numel()} entries, expected {(B - 1) * idx_batch_stride + Nout}")
+    if dx is None:
+        if accumulate:
+            raise ValueError("accumulate needs dx")
+        dx = torch.zeros_like(x)
+    _shape(dx, x.shape, "dx")
+    dgamma = dbeta = None
+    if weight_grads:
+        dgamma, dbeta = (torch.empty(D, dtype=torch.float32, device=x.device) for _ in range(2))
+        if workspace is None:
+            workspace = torch.empty(ssam_ln_gather_backward_workspace_bytes(B, Nout, D), dtype=torch.uint8, device=x.device)
+    _one_device(x=x, idx=idx, gamma=gamma, dy=dy, dx=dx, workspace=workspace)
+    _check("ssam_ln_gather_backward", lib().ssam_ln_gather_backward(
+        *ptrs, _bf(dx, "dx"), C.c_int(1 if accumulate else 0), _f32(dgamma, "dgamma"), _f32(dbeta, "dbeta"),
+        C.c_int(B), C.c_int(Nin), C.c_int(Nout), C.c_int(D), _dev(workspace, torch.uint8, "workspace"),
+        C.c_size_t(0 if workspace is None else workspace.numel()), _stream()))
+    return dx, dgamma, dbeta
+
+
+CHECKPOINT_COLUMNS = 64       # columns of a row that share a scale
+
+
+def _checkpoint(like, codes, scales):
+    D = like.shape[-1]
+    lead = tuple(like.shape[:-1])
+    if codes is None:
+        codes = torch.empty((*lead, D), dtype=torch.int8, device=like.device)
+    if scales is None:
+        scales = torch.empty((*lead, -(-D // CHECKPOINT_COLUMNS)), dtype=torch.float32, device=like.device)
+    _shape(codes, (*lead, D), "codes")
+    _shape(scales, (*lead, -(-D // CHECKPOINT_COLUMNS)), "scales")
+    _one_device(activation=like, codes=codes, scales=scales)
+    return codes, scales, C.c_long(like.numel() // D if D else 0), C.c_int(D)
+
+
+def ssam_checkpoint_store(x, codes=None, scales=None):
+    """x [..., D] bf16 -> (codes [..., D] int8, scales [..., ceil(D/64)] fp32)."""
+    px = _bf(x, "x")
+    codes, scales, rows, D = _checkpoint(x, codes, scales)
+    _check("ssam_checkpoint_store", lib().ssam_checkpoint_store(px, _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), rows, D, _stream()))
+    return codes, scales
+
+
+def ssam_checkpoint_restore(codes, scales, x=None):
+    """The bf16 activation [..., D] that codes and scales hold."""
+    pc, ps = _dev(codes, torch.int8, "codes"), _f32(scales, "scales")
+    if x is None:
+        x = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
+    px = _bf(x, "x")
+    _, _, rows, D = _checkpoint(x, codes, scales)
+    _check("ssam_checkpoint_restore", lib().ssam_checkpoint_restore(pc, ps, px, rows, D, _stream()))
+    return x
+
+
+def ssam_gelu_checkpoint(h, a=None, codes=None, scales=None):
+    """h [..., D] bf16 -> (a = gelu(h) bf16, codes, scales of h); a may be h."""
+    ph = _bf(h, "h")
+    if a is None:
+        a = torch.empty_like(h)
+    _shape(a, h.shape, "a")
+    pa = _bf(a, "a")
+    codes, scales, rows, D = _checkpoint(h, codes, scales)
+    _one_device(a=a)
+    _check("ssam_gelu_checkpoint", lib().ssam_gelu_checkpoint(ph, pa, _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), rows, D, _stream()))
+    return a, codes, scales
+
+
+def ssam_gelu_backward(codes, scales, da, dh=None, a=None, activation=True):
+    """Gradient da of gelu(h) -> (dh, a): the gradient of h and, unless activation is False, gelu of the h that codes and scales hold.  dh may be da."""
+    pc, ps, pd = _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), _bf(da, "da")
+    if dh is None:
+        dh = torch.empty_like(da)
+    if a is None and activation:
+        a = torch.empty_like(da)
+    _shape(dh, da.shape, "dh")
+    _shape(a, da.shape, "a")
+    _, _, rows, D = _checkpoint(da, codes, scales)
+    _one_device(dh=dh, a=a)
+    _check("ssam_gelu_backward", lib().ssam_gelu_backward(pc, ps, pd, _bf(dh, "dh"), _bf(a, "a"), rows, D, _stream()))
+    return dh, a
 
 
 # ------------------------------------------------------------------ instrumentation
