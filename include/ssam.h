@@ -427,6 +427,24 @@ int ssam_neck(const void *x, const void *w1, const float *ln1_g, const float *ln
 /* Gradients: what a training step of the block needs beside the calls above  */
 /* ------------------------------------------------------------------------- */
 
+/* Gradients of ssam_sparse_attention, which forms the probabilities again.  q, k, v, row_stride, rel_h, rel_w, sigma,
+ * sigma_group_stride, out_rows, groups, S, w, h, d, mask_block, r, scale as in the forward call; out: its result; dout
+ * dev bf16: the gradient of it, rows as in out.  A query that out_rows drops (negative) has no gradient and gives none.
+ *   dq, dk, dv      dev bf16, element (g, p, head, c) at ptr[(g*S+p)*grad_stride + head*d + c], all of them written (a
+ *                   packed [groups][S][3][h][d] buffer: grad_stride = 3*h*d, dk = dq + h*d, dv = dq + 2*h*d)
+ *   drel_h, drel_w  dev bf16 [(2w-1)][d], written: sums over all groups, heads and queries; both NULL: not wanted
+ * No output may overlap an input or the workspace (dev, >= ..._workspace_bytes; about 4 bytes * 32, 64, 128 or 256, the
+ * next multiple from 2w, per query and head).  Sums are fp32, probabilities and their gradients bf16 where they are
+ * multiplied, bias entries fp16 (up to +-45400 as a logit); no atomics: the same inputs give the same bits.
+ * Built for the sizes of the forward call (w <= 128, d in {16, 32, 64, 80}), else SSAM_EUNSUPPORTED. */
+size_t ssam_sparse_attention_backward_workspace_bytes(int groups, int S, int w, int h, int d);
+int ssam_sparse_attention_backward(const void *q, const void *k, const void *v, long row_stride,
+                                   const void *rel_h, const void *rel_w, const int32_t *sigma,
+                                   long sigma_group_stride, const void *out, const void *dout, const int32_t *out_rows,
+                                   void *dq, void *dk, void *dv, long grad_stride, void *drel_h, void *drel_w,
+                                   int groups, int S, int w, int h, int d, int mask_block, double r, float scale,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
 /* Gradient of ssam_ln_gather.  With h = (x - mean) * rstd of the row that output row p was made from, g = dy * gamma:
  *   dx row  (+)= rstd * (g - mean_D(g) - h * mean_D(g * h)),  dgamma = sum dy * h,  dbeta = sum dy  (sums over all rows).
  * x, idx, idx_batch_stride, gamma, eps, B, Nin, Nout, D as in the forward call; dy dev bf16 [B][Nout][D].

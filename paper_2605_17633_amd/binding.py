@@ -55,7 +55,7 @@ def lib():
         for n in ("ssam_score_tokens_workspace_bytes", "ssam_routed_mlp_workspace_bytes",
                   "ssam_encoder_block_workspace_bytes", "ssam_encoder_workspace_bytes", "ssam_linear_workspace_bytes",
                   "ssam_patch_embed_workspace_bytes", "ssam_neck_workspace_bytes",
-                  "ssam_ln_gather_backward_workspace_bytes"):
+                  "ssam_ln_gather_backward_workspace_bytes", "ssam_sparse_attention_backward_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         L.ssam_probe_mfma_flops.restype = C.c_double
         _lib = L
@@ -552,6 +552,43 @@ def _one_device(**tensors):
 def _shape(t, want, name):
     if t is not None and tuple(t.shape) != tuple(want):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(want)}")
+
+
+def ssam_sparse_attention_backward_workspace_bytes(groups, S, w, h, d) -> int:
+    return lib().ssam_sparse_attention_backward_workspace_bytes(C.c_int(groups), C.c_int(S), C.c_int(w), C.c_int(h), C.c_int(d))
+
+
+def ssam_sparse_attention_backward(qkv, rel_h, rel_w, sigma, w, mask_block, r, out, dout, scale=None, out_rows=None, dqkv=None,
+                                   table_grads=True, workspace=None):
+    """qkv, rel_h, rel_w, sigma, out_rows as given to ssam_sparse_attention, out its result, dout the gradient of that
+    -> (dqkv [groups,S,3,h,d], drel_h, drel_w [2w-1,d]) bf16."""
+    groups, S, three, h, d = qkv.shape
+    assert three == 3
+    if scale is None:
+        scale = d ** -0.5
+    if dqkv is None:
+        dqkv = torch.empty_like(qkv)
+    drel_h = drel_w = None
+    if table_grads:
+        drel_h, drel_w = torch.empty_like(rel_h), torch.empty_like(rel_w)
+    if workspace is None:
+        workspace = torch.empty(ssam_sparse_attention_backward_workspace_bytes(groups, S, w, h, d), dtype=torch.uint8, device=qkv.device)
+    _bf(qkv, "qkv"), _bf(dqkv, "dqkv")
+    for name, t, want in (("rel_h", rel_h, (2 * w - 1, d)), ("rel_w", rel_w, (2 * w - 1, d)), ("dqkv", dqkv, qkv.shape), ("dout", dout, out.shape)):
+        _shape(t, want, name)
+    if sigma.numel() != (groups if sigma.dim() == 2 else 1) * S:
+        raise ValueError(f"sigma: shape {tuple(sigma.shape)}, expected [{S}] or [{groups}, {S}]")
+    if out.shape[-1] != h * d or (out_rows is None and out.numel() != groups * S * h * d) or (out_rows is not None and out_rows.numel() != groups * S):
+        raise ValueError("out: rows of h*d, one for every query, or out_rows with a row of out for every query")
+    _one_device(qkv=qkv, rel_h=rel_h, rel_w=rel_w, sigma=sigma, out=out, dout=dout, out_rows=out_rows, dqkv=dqkv, workspace=workspace)
+    at, grad, step = qkv.data_ptr(), dqkv.data_ptr(), 2 * h * d
+    _check("ssam_sparse_attention_backward", lib().ssam_sparse_attention_backward(
+        C.c_void_p(at), C.c_void_p(at + step), C.c_void_p(at + 2 * step), C.c_long(3 * h * d), _bf(rel_h, "rel_h"), _bf(rel_w, "rel_w"),
+        _i32(sigma, "sigma"), C.c_long(S if sigma.dim() == 2 else 0), _bf(out, "out"), _bf(dout, "dout"), _i32(out_rows, "out_rows"),
+        C.c_void_p(grad), C.c_void_p(grad + step), C.c_void_p(grad + 2 * step), C.c_long(3 * h * d), _bf(drel_h, "drel_h"), _bf(drel_w, "drel_w"),
+        C.c_int(groups), C.c_int(S), C.c_int(w), C.c_int(h), C.c_int(d), C.c_int(mask_block), C.c_double(r), C.c_float(scale),
+        _dev(workspace, torch.uint8, "workspace"), C.c_size_t(workspace.numel()), _stream()))
+    return dqkv, drel_h, drel_w
 
 
 def ssam_ln_gather_backward_workspace_bytes(B, Nout, D) -> int:

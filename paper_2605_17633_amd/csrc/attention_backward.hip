@@ -54,9 +54,13 @@ struct BwdCfg {
     static constexpr int KP = D + EW + 8, VP = D + 8;        // LDS pitches (elements): odd in 16-byte units
     static constexpr int TP = EW + 8;                        // of bias entries
     static constexpr int RP = 2 * WK + 8;                    // of G at relative positions, one table
+    static constexpr int ROW_KEYS = NT < 8 ? 64 : 32;        // keys of a stage of the row kernel
+    static constexpr bool KEEP = NT < 8;                     // a wave's queries, dO and bias entries stay in registers, else in LDS
 };
-constexpr int ROW_KEYS = 64;     // keys of a stage of the row kernel
 constexpr int COL_QUERIES = 32;  // queries of a stage of the column kernel
+
+// bit 23 of the mode register: fp16 results past the range are clamped instead of rounded to infinity (which would make NaNs of the zeros of E)
+__device__ __forceinline__ void clamp_fp16() { __builtin_amdgcn_s_setreg(1 | 23 << 6 | (1 - 1) << 11, 1); }
 
 // MFMA passes done before results are read under predicates (see the forward kernels)
 __device__ __forceinline__ void mfma_settle()
@@ -83,7 +87,8 @@ __device__ __forceinline__ f32x16 zero16()
 __device__ __forceinline__ bf16x8 transposed(const bf16 *block, int pitch, int t, int tile, int last)
 {
     const int lane = threadIdx.x & 63, li = lane & 15;
-    const int col = min(tile * 32 + 16 * ((lane >> 4) & 1) + 4 * (li & 3), last);
+    int col = tile * 32 + 16 * ((lane >> 4) & 1) + 4 * (li & 3);
+    if (tile * 32 + 28 > last) col = min(col, last);         // (known at compile time: the others' addresses differ by constants)
     const bf16 *p = block + (16 * t + 4 * (lane >> 5) + (li >> 2)) * pitch + col;
     const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(p));
     const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(p + 8 * pitch));
@@ -127,8 +132,8 @@ template <int D, int NT>
 __host__ __device__ constexpr size_t rows_lds_bytes(int nrel)
 {
     using C = BwdCfg<D, NT>;
-    const size_t stage = (size_t)ROW_KEYS * (C::KP + C::VP) * 2;
     const size_t tables = (size_t)4 * 32 * C::TP * 2;
+    const size_t stage = (size_t)C::ROW_KEYS * (C::KP + C::VP) * 2 + (C::KEEP ? 0 : tables + (size_t)4 * 32 * 2 * C::VP * 2);
     const size_t end = (size_t)4 * 32 * C::RP * 2 + (size_t)(nrel + 31) / 16 * 16 * C::VP * 2;
     const size_t rows = (size_t)4 * 32 * C::VP * 2;
     size_t m = stage > tables ? stage : tables;
@@ -146,6 +151,7 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
     // the tiles of one (group, head) run on one XCD (workgroup b sits on XCD b & 7), whose L2 then serves the re-reads of its K and V
     const int tile = (blockIdx.x >> 3) % tiles, gh = ((blockIdx.x >> 3) / tiles) * 8 + (blockIdx.x & 7);
     if (gh >= P.n_gh) return;
+    clamp_fp16();
     const int grp = gh / P.h, head = gh - grp * P.h;
     const int S = P.S, w = P.w, nrel = 2 * w - 1;
     const int q0 = tile * 128, qpos = q0 + wave * 32 + l32;
@@ -197,62 +203,72 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int p = p0 - 8 * (r >> 2) - (r & 3);
-                // a bias past the range of fp16 (45000 as a logit) is cut: an infinity would make NaNs of the zeros of E
-                if ((unsigned)p < (unsigned)w) tq[tab * C::WK + p] = (_Float16)__builtin_amdgcn_fmed3f(u[r] * LOG2E, -65504.f, 65504.f);
+                if ((unsigned)p < (unsigned)w) tq[tab * C::WK + p] = (_Float16)(u[r] * LOG2E);        // up to 45400 as a logit
             }
         }
     wave_lds_fence();
-    f16x8 bt[C::ES];
+    f16x8 bt[C::KEEP ? C::ES : 1];
+    if constexpr (C::KEEP)
 #pragma unroll
-    for (int c = 0; c < C::ES; ++c) bt[c] = *reinterpret_cast<const f16x8 *>(tq + 16 * c + 8 * half);
+        for (int c = 0; c < C::ES; ++c) bt[c] = *reinterpret_cast<const f16x8 *>(tq + 16 * c + 8 * half);
     if (qpos < S) {
         _Float16 *to = P.tab + ((long)gh * S + qpos) * C::EW + 8 * half;
 #pragma unroll
-        for (int c = 0; c < C::ES; ++c) *reinterpret_cast<f16x8 *>(to + 16 * c) = bt[c];
+        for (int c = 0; c < C::ES; ++c) *reinterpret_cast<f16x8 *>(to + 16 * c) = *reinterpret_cast<const f16x8 *>(tq + 16 * c + 8 * half);
     }
     __syncthreads();
 
     // stages of 64 keys: the dense prefix, then (where a wave has a diagonal tile behind it) the workgroup's own 128
-    bf16 *Ks = reinterpret_cast<bf16 *>(smem), *Vs = Ks + ROW_KEYS * C::KP;
-    const int pre = min(P.n_pre * P.mask_block, S), pre_stages = ssam_div_up(pre, ROW_KEYS);
+    bf16 *Ks = reinterpret_cast<bf16 *>(smem) + (C::KEEP ? 0 : 4 * 32 * (C::TP + 2 * C::VP)), *Vs = Ks + C::ROW_KEYS * C::KP;
+    // where registers are short, the wave's queries and dO lie behind the bias entries
+    bf16 *qs = reinterpret_cast<bf16 *>(smem) + 4 * 32 * C::TP + (wave * 32 + l32) * 2 * C::VP + half * 8, *os = qs + C::VP;
+    if constexpr (!C::KEEP)
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks) {
+            *reinterpret_cast<bf16x8 *>(qs + ks * 16) = qf[ks];
+            *reinterpret_cast<bf16x8 *>(os + ks * 16) = of[ks];
+        }
+    auto query = [&](int ks) { return C::KEEP ? qf[ks] : *reinterpret_cast<const bf16x8 *>(qs + ks * 16); };
+    auto upstream = [&](int ks) { return C::KEEP ? of[ks] : *reinterpret_cast<const bf16x8 *>(os + ks * 16); };
+    const int pre = min(P.n_pre * P.mask_block, S), pre_stages = (pre + C::ROW_KEYS - 1) / C::ROW_KEYS;
     const int own = (q0 + wave * 32) / P.mask_block;                                  // mask tile of the wave's queries
     const bool any_diagonal = min(q0 + 127, S - 1) / P.mask_block >= P.n_pre;
-    const int stages = pre_stages + (any_diagonal ? ssam_div_up(min(128, S - q0), ROW_KEYS) : 0);
+    const int stages = pre_stages + (any_diagonal ? (min(128, S - q0) + C::ROW_KEYS - 1) / C::ROW_KEYS : 0);
     const bool alive = q0 + wave * 32 < S;
 
-    for (int i = tid; i < ROW_KEYS * (C::EW / 8); i += 256)                          // E starts empty
+    for (int i = tid; i < C::ROW_KEYS * (C::EW / 8); i += 256)                          // E starts empty
         *reinterpret_cast<uint4 *>(Ks + (i / (C::EW / 8)) * C::KP + D + (i % (C::EW / 8)) * 8) = make_uint4(0, 0, 0, 0);
 
-    constexpr int CH = D / 8, NLOAD = (ROW_KEYS * CH + 255) / 256;
+    constexpr int CH = D / 8, NLOAD = (C::ROW_KEYS * CH + 255) / 256;
     u32x4 kr[NLOAD], vr[NLOAD];
     int cell_next = -1;
     const bf16 *kbase = P.k + (long)grp * S * P.row_stride + (long)head * D, *vbase = P.v + (long)grp * S * P.row_stride + (long)head * D;
-    auto stage_key = [&](int s) { return s < pre_stages ? s * ROW_KEYS : q0 + (s - pre_stages) * ROW_KEYS; };
+    auto stage_key = [&](int s) { return s < pre_stages ? s * C::ROW_KEYS : q0 + (s - pre_stages) * C::ROW_KEYS; };
     auto load = [&](int s) {
         const int key0 = stage_key(s);
 #pragma unroll
         for (int i = 0; i < NLOAD; ++i) {
             const int id = tid + 256 * i, row = id / CH, c = id - row * CH;
             kr[i] = vr[i] = u32x4{ 0, 0, 0, 0 };
-            if (id < ROW_KEYS * CH && key0 + row < S) {
+            if (id < C::ROW_KEYS * CH && key0 + row < S) {
                 const long at = (long)(key0 + row) * P.row_stride + c * 8;
                 kr[i] = *reinterpret_cast<const u32x4 *>(kbase + at);
                 vr[i] = *reinterpret_cast<const u32x4 *>(vbase + at);
             }
         }
-        if (tid < ROW_KEYS) cell_next = key0 + tid < S ? sigma[key0 + tid] : -1;
+        if (tid < C::ROW_KEYS) cell_next = key0 + tid < S ? sigma[key0 + tid] : -1;
     };
     int one_row = -1, one_col = -1;                                                   // where this thread's key has its ones
     auto store = [&]() {
 #pragma unroll
         for (int i = 0; i < NLOAD; ++i) {
             const int id = tid + 256 * i, row = id / CH, c = id - row * CH;
-            if (id < ROW_KEYS * CH) {
+            if (id < C::ROW_KEYS * CH) {
                 *reinterpret_cast<u32x4 *>(Ks + row * C::KP + c * 8) = kr[i];
                 *reinterpret_cast<u32x4 *>(Vs + row * C::VP + c * 8) = vr[i];
             }
         }
-        if (tid < ROW_KEYS) {
+        if (tid < C::ROW_KEYS) {
             uint16_t *e = reinterpret_cast<uint16_t *>(Ks + tid * C::KP + D);
             if (one_row >= 0) e[one_row] = e[one_col] = 0;
             one_row = -1;
@@ -276,22 +292,24 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
         const int key0 = stage_key(s);
         if (s + 1 < stages) load(s + 1);
 #pragma unroll
-        for (int b = 0; b < ROW_KEYS / 32; ++b) {
+        for (int b = 0; b < C::ROW_KEYS / 32; ++b) {
             const int kb = key0 + 32 * b;
             const bool active = alive && kb < S && (s < pre_stages ? kb < pre : own >= P.n_pre && kb / P.mask_block == own);
-            if (!active) continue;                           // wave-uniform
+            if (!active) continue;                           // the same for the whole wave
             const bf16 *kblk = Ks + 32 * b * C::KP, *vblk = Vs + 32 * b * C::VP;
             f32x16 sc = zero16(), bias = zero16(), dp = zero16();
 #pragma unroll
             for (int ks = 0; ks < C::KS; ++ks)
-                sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(kblk + l32 * C::KP + ks * 16 + half * 8), qf[ks], sc, 0, 0, 0);
+                sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(kblk + l32 * C::KP + ks * 16 + half * 8), query(ks), sc, 0, 0, 0);
 #pragma unroll
-            for (int c = 0; c < C::ES; ++c)
-                bias = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(kblk + l32 * C::KP + D + c * 16 + half * 8), bt[c], bias, 0, 0, 0);
+            for (int c = 0; c < C::ES; ++c) {
+                if (!C::KEEP && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                bias = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(kblk + l32 * C::KP + D + c * 16 + half * 8),
+                                                              C::KEEP ? bt[C::KEEP ? c : 0] : *reinterpret_cast<const f16x8 *>(tq + 16 * c + 8 * half), bias, 0, 0, 0);
+            }
 #pragma unroll
             for (int ks = 0; ks < C::KS; ++ks)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(vblk + l32 * C::VP + ks * 16 + half * 8), of[ks], dp, 0, 0, 0);
-            mfma_settle();
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(vblk + l32 * C::VP + ks * 16 + half * 8), upstream(ks), dp, 0, 0, 0);
             float mx = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -307,9 +325,11 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
                 m = to;
                 l *= alpha;
 #pragma unroll
-                for (int t = 0; t < C::CT; ++t)
+                for (int t = 0; t < C::CT; ++t) {
+                    if (!C::KEEP) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[t][r] *= alpha;
+                }
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -321,7 +341,11 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
             for (int t = 0; t < 2; ++t) {
                 const bf16x8 ds = half_of(dp, t);
 #pragma unroll
-                for (int c = 0; c < C::CT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(kblk, C::KP, t, c, D + C::EW - 4), ds, acc[c], 0, 0, 0);
+                for (int c = 0; c < C::CT; ++c) {
+                    // eleven tiles of accumulators leave no registers for operands read further ahead
+                    if (!C::KEEP && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(kblk, C::KP, t, c, D + C::EW - 4), ds, acc[c], 0, 0, 0);
+                }
             }
         }
     }
@@ -331,18 +355,38 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
         P.stat[(long)gh * S + qpos] = orow < 0 ? make_float2(-INFINITY, 0.f) : make_float2(-m - __builtin_amdgcn_logf(l), delta);
     const float inv = 1.f / l;
 #pragma unroll
-    for (int c = 0; c < C::CT; ++c)
+    for (int c = 0; c < C::CT; ++c) {
+        if (!C::KEEP) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const float f = c * 32 + 8 * g < D ? inv * P.scale : inv * 128.f;       // (a group of eight columns is on one side)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[c][4 * g + e] = alive ? acc[c][4 * g + e] * f : 0.f;
         }
+    }
 
     // dQ += G at relative positions . rel, one table after the other
     bf16 *gr = reinterpret_cast<bf16 *>(smem) + wave * 32 * C::RP, *rel = reinterpret_cast<bf16 *>(smem) + 4 * 32 * C::RP;
     bf16 *mine = gr + l32 * C::RP;
     const int relrows = (nrel + 15) / 16 * 16;
+    __syncthreads();
+    if (P.gsum) {                                            // G as it is, for the tables' gradient
+#pragma unroll
+        for (int c = 0; c < C::CT; ++c)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = c * 32 + 8 * g - D;
+                if (col < 0 || col >= C::EW) continue;
+                bf16x4 v = { (bf16)acc[c][4 * g], (bf16)acc[c][4 * g + 1], (bf16)acc[c][4 * g + 2], (bf16)acc[c][4 * g + 3] };
+                *reinterpret_cast<bf16x4 *>(mine + col + 4 * half) = v;
+            }
+        wave_lds_fence();
+        for (int i = lane; i < 32 * (C::EW / 8); i += 64) {
+            const int r = i / (C::EW / 8), c = i % (C::EW / 8), at = q0 + wave * 32 + r;
+            if (at < S) *reinterpret_cast<uint4 *>(P.gsum + ((long)gh * S + at) * C::EW + c * 8) = *reinterpret_cast<const uint4 *>(gr + r * C::RP + c * 8);
+        }
+        wave_lds_fence();
+    }
 #pragma unroll
     for (int tab = 0; tab < 2; ++tab) {
         __syncthreads();
@@ -370,11 +414,383 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
             const bf16x8 g8 = { a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3] };
 #pragma unroll
             for (int dt = 0; dt < C::DT; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(rel + 16 * t * C::VP, C::VP, 0, dt, D - 4), g8, acc[dt], 0, 0, 0);
-            // (of a last tile that D fills by half the rest are entries of G, which the operand's repeated columns change: GW's is taken
-            // before, see below)
+            // (the half of a last tile that D does not fill holds entries of GH, which are no longer needed)
         }
         mfma_settle();
     }
+    __syncthreads();
     store_rows<D>(acc, reinterpret_cast<bf16 *>(smem) + wave * 32 * C::VP, P.dq + (long)grp * S * P.grad_stride + (long)head * D, P.grad_stride, qpos < S ? qpos : -1);
 }
+
+// ---------------------------------------------------------------- columns
+template <int D, int NT>
+__host__ __device__ constexpr size_t columns_lds_bytes()
+{
+    using C = BwdCfg<D, NT>;
+    const size_t stage = (size_t)COL_QUERIES * (2 * C::VP + C::TP) * 2 + COL_QUERIES * 8;
+    const size_t rows = (size_t)4 * 32 * C::VP * 2;
+    return stage > rows ? stage : rows;
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(256, NT >= 8 || D == 80 ? 1 : 2)
+attn_backward_columns_kernel(BwdParams P, int tiles)
+{
+    using C = BwdCfg<D, NT>;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+    const int tile = (blockIdx.x >> 3) % tiles, gh = ((blockIdx.x >> 3) / tiles) * 8 + (blockIdx.x & 7);
+    if (gh >= P.n_gh) return;
+    const int grp = gh / P.h, head = gh - grp * P.h;
+    const int S = P.S, w = P.w;
+    const int k0 = tile * 128, kb = k0 + wave * 32, kpos = kb + l32;
+    bf16x8 kf[C::KS], vf[C::KS];
+    f16x8 ef[C::ES];
+    {
+        const int at = min(kpos, S - 1);                     // keys past the end repeat the last one; their results are not stored
+        const long o = ((long)grp * S + at) * P.row_stride + (long)head * D + half * 8;
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks) {
+            kf[ks] = *reinterpret_cast<const bf16x8 *>(P.k + o + ks * 16);
+            vf[ks] = *reinterpret_cast<const bf16x8 *>(P.v + o + ks * 16);
+        }
+        const int cell = P.sigma[(long)grp * P.sigma_stride + at], row = cell / w, col = cell - row * w;
+#pragma unroll
+        for (int c = 0; c < C::ES; ++c) {
+            const int i = (16 * c < C::WK ? row : col + C::WK) - 16 * c - 8 * half;
+            u32x4 e;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = i >> 1 == j ? (i & 1 ? 0x3c000000u : 0x3c00u) : 0u;
+            ef[c] = __builtin_bit_cast(f16x8, e);
+        }
+    }
+    f32x16 dk[C::DT], dv[C::DT];
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t) { dk[t] = zero16(); dv[t] = zero16(); }
+
+    bf16 *Qs = reinterpret_cast<bf16 *>(smem), *Os = Qs + COL_QUERIES * C::VP;
+    _Float16 *Ts = reinterpret_cast<_Float16 *>(Os + COL_QUERIES * C::VP);
+    float *Ls = reinterpret_cast<float *>(Ts + COL_QUERIES * C::TP), *Ds = Ls + COL_QUERIES;
+
+    // a key of the dense prefix is seen by every query, another by those of its own tile
+    const bool prefix = kb / P.mask_block < P.n_pre, any_prefix = k0 / P.mask_block < P.n_pre, alive = kb < S;
+    const int first = any_prefix ? 0 : k0, last = any_prefix ? S : min(k0 + 128, S);
+    constexpr int CH = D / 8, NQ = (COL_QUERIES * CH + 255) / 256, NB = (COL_QUERIES * (C::EW / 8) + 255) / 256;
+    u32x4 qr[NQ], dr[NQ], tr[NB];
+    float2 st = make_float2(0.f, 0.f);
+    auto load = [&](int q0) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const int id = tid + 256 * i, row = id / CH, c = id - row * CH;
+            qr[i] = dr[i] = u32x4{ 0, 0, 0, 0 };
+            if (id < COL_QUERIES * CH && q0 + row < S) {
+                const long slot = (long)grp * S + q0 + row;
+                const int orow = P.out_rows ? P.out_rows[slot] : 0;
+                if (orow >= 0) {
+                    qr[i] = *reinterpret_cast<const u32x4 *>(P.q + slot * P.row_stride + (long)head * D + c * 8);
+                    dr[i] = *reinterpret_cast<const u32x4 *>(P.dout + (P.out_rows ? (long)orow : slot) * ((long)P.h * D) + (long)head * D + c * 8);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int id = tid + 256 * i, row = id / (C::EW / 8), c = id % (C::EW / 8);
+            tr[i] = u32x4{ 0, 0, 0, 0 };
+            if (id < COL_QUERIES * (C::EW / 8) && q0 + row < S) tr[i] = *reinterpret_cast<const u32x4 *>(P.tab + ((long)gh * S + q0 + row) * C::EW + c * 8);
+        }
+        if (tid < COL_QUERIES) st = q0 + tid < S ? P.stat[(long)gh * S + q0 + tid] : make_float2(-INFINITY, 0.f);
+    };
+    load(first);
+    for (int q0 = first; q0 < last; q0 += COL_QUERIES) {
+        LDS_BARRIER();
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const int id = tid + 256 * i, row = id / CH, c = id - row * CH;
+            if (id < COL_QUERIES * CH) {
+                *reinterpret_cast<u32x4 *>(Qs + row * C::VP + c * 8) = qr[i];
+                *reinterpret_cast<u32x4 *>(Os + row * C::VP + c * 8) = dr[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int id = tid + 256 * i, row = id / (C::EW / 8), c = id % (C::EW / 8);
+            if (id < COL_QUERIES * (C::EW / 8)) *reinterpret_cast<u32x4 *>(Ts + row * C::TP + c * 8) = tr[i];
+        }
+        if (tid < COL_QUERIES) { Ls[tid] = st.x; Ds[tid] = st.y; }
+        LDS_BARRIER();
+        if (q0 + COL_QUERIES < last) load(q0 + COL_QUERIES);
+        if (!alive || !(prefix || q0 / P.mask_block == kb / P.mask_block)) continue;     // the same for the whole wave
+        // result rows are queries: register r <-> query 8 (r >> 2) + 4 half + (r & 3); the bias begins at -log2 sum exp
+        f32x16 p, s = zero16(), ds = zero16();
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(Ls + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[4 * g + e] = v[e];
+        }
+#pragma unroll
+        for (int c = 0; c < C::ES; ++c)
+            p = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(Ts + l32 * C::TP + 16 * c + 8 * half), ef[c], p, 0, 0, 0);
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(Qs + l32 * C::VP + 16 * ks + 8 * half), kf[ks], s, 0, 0, 0);
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks)
+            ds = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(Os + l32 * C::VP + 16 * ks + 8 * half), vf[ks], ds, 0, 0, 0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(Ds + 8 * g + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * g + e;
+                p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], P.scale_log2e, p[r]));
+                ds[r] = p[r] * (ds[r] - v[e]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const bf16x8 pf = half_of(p, t), df = half_of(ds, t);
+#pragma unroll
+            for (int dt = 0; dt < C::DT; ++dt) {
+                dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(Os, C::VP, t, dt, D - 4), pf, dv[dt], 0, 0, 0);
+                dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(Qs, C::VP, t, dt, D - 4), df, dk[dt], 0, 0, 0);
+            }
+        }
+    }
+    mfma_settle();
+    __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dk[dt][r] *= P.scale;
+    bf16 *scratch = reinterpret_cast<bf16 *>(smem) + wave * 32 * C::VP;
+    const long to = (long)grp * S * P.grad_stride + (long)head * D;
+    const int row = kpos < S ? kpos : -1;
+    store_rows<D>(dk, scratch, P.dk + to, P.grad_stride, row);
+    store_rows<D>(dv, scratch, P.dv + to, P.grad_stride, row);
+}
+
+// ---------------------------------------------------------------- tables
+// A unit is 32 queries of one (group, head).  A workgroup adds up those of a slice in registers: result [relative position of both tables][feature].
+template <int D, int NT>
+__host__ __device__ constexpr size_t tables_lds_bytes()
+{
+    using C = BwdCfg<D, NT>;
+    return (size_t)32 * (4 * C::WK + 8 + C::VP) * 2;
+}
+
+template <int D, int NT>
+__global__ void __launch_bounds__(256, NT >= 8 ? 1 : 2)
+attn_backward_tables_kernel(BwdParams P, int units_per_gh, long units, float *__restrict__ parts)
+{
+    using C = BwdCfg<D, NT>;
+    constexpr int TT = 4 * C::WK / 32;                       // 32-row tiles of relative positions
+    constexpr int MINE = (TT + 3) / 4, GP = 4 * C::WK + 8;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    bf16 *Gs = reinterpret_cast<bf16 *>(smem), *Qs = Gs + 32 * GP;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+    const int S = P.S, w = P.w;
+    f32x16 acc[MINE][C::DT];
+#pragma unroll
+    for (int i = 0; i < MINE; ++i)
+#pragma unroll
+        for (int dt = 0; dt < C::DT; ++dt) acc[i][dt] = zero16();
+    const long per = (units + gridDim.x - 1) / gridDim.x, u1 = min((long)(blockIdx.x + 1) * per, units);
+    for (long u = blockIdx.x * per; u < u1; ++u) {
+        const int gh = (int)(u / units_per_gh), q0 = (int)(u - (long)gh * units_per_gh) * 32, grp = gh / P.h, head = gh - grp * P.h;
+        __syncthreads();
+        for (int i = tid; i < 32 * (GP / 8); i += 256) *reinterpret_cast<uint4 *>(Gs + i * 8) = make_uint4(0, 0, 0, 0);
+        constexpr int CH = D / 8;
+        for (int i = tid; i < 32 * CH; i += 256) {
+            const int row = i / CH, c = i - row * CH;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (q0 + row < S) {
+                const long slot = (long)grp * S + q0 + row;
+                if (!P.out_rows || P.out_rows[slot] >= 0) v = *reinterpret_cast<const uint4 *>(P.q + slot * P.row_stride + (long)head * D + c * 8);
+            }
+            *reinterpret_cast<uint4 *>(Qs + row * C::VP + c * 8) = v;
+        }
+        __syncthreads();
+        for (int i = tid; i < 32 * (C::EW / 8); i += 256) {
+            const int row = i / (C::EW / 8), c = i % (C::EW / 8), tab = c * 8 >= C::WK, y0 = c * 8 - tab * C::WK;
+            if (q0 + row >= S || y0 >= w) continue;
+            const int cell = P.sigma[(long)grp * P.sigma_stride + q0 + row], r = cell / w, t0 = (tab ? cell - r * w : r) + w - 1 - y0;
+            const bf16x8 g = *reinterpret_cast<const bf16x8 *>(P.gsum + ((long)gh * S + q0 + row) * C::EW + c * 8);
+            bf16 *to = Gs + row * GP + tab * 2 * C::WK + t0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (y0 + e < w) to[-e] = g[e];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            bf16x8 qt[C::DT];
+#pragma unroll
+            for (int dt = 0; dt < C::DT; ++dt) qt[dt] = transposed(Qs, C::VP, t, dt, D - 4);
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                if (wave * MINE + i >= TT) continue;
+                const bf16x8 g = transposed(Gs, GP, t, wave * MINE + i, GP - 4);
+#pragma unroll
+                for (int dt = 0; dt < C::DT; ++dt) acc[i][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g, qt[dt], acc[i][dt], 0, 0, 0);
+            }
+        }
+    }
+    mfma_settle();
+    // result: lane <-> feature, register <-> relative position
+    float *to = parts + (long)blockIdx.x * 4 * C::WK * D;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i)
+#pragma unroll
+        for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int t = (wave * MINE + i) * 32 + 8 * (r >> 2) + 4 * half + (r & 3), c = dt * 32 + l32;
+                if (wave * MINE + i < TT && c < D) to[(long)t * D + c] = acc[i][dt][r];
+            }
+}
+
+// [n][2][2 WK][D] sums of slices -> bf16 tables of nrel rows.  A workgroup adds up 32 columns: eight lanes with 16 bytes each, 32 slices of the n.
+__global__ void __launch_bounds__(256)
+attn_backward_table_sums_kernel(const float4 *__restrict__ parts, int n, int table, int used, bf16 *__restrict__ drel_h, bf16 *__restrict__ drel_w)
+{
+    __shared__ float4 lds[256];
+    const int c = threadIdx.x & 7, slice = threadIdx.x >> 3;
+    const int col = (blockIdx.x * 8 + c) * 4;                // element of the table
+    const bool in = col < used;
+    const long at = ((long)blockIdx.y * table + min(col, used - 4)) / 4;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int r = slice; r < n; r += 32) {
+        const float4 t = parts[(long)r * 2 * table / 4 + at];
+        a.x += t.x; a.y += t.y; a.z += t.z; a.w += t.w;
+    }
+    lds[threadIdx.x] = a;
+    __syncthreads();
+#pragma unroll
+    for (int half = 16; half > 0; half >>= 1) {
+        if (slice < half) {
+            const float4 t = lds[threadIdx.x + half * 8];
+            a.x += t.x; a.y += t.y; a.z += t.z; a.w += t.w;
+            lds[threadIdx.x] = a;
+        }
+        __syncthreads();
+    }
+    if (slice == 0 && in) *reinterpret_cast<uint2 *>((blockIdx.y ? drel_w : drel_h) + col) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+}
+
+// ---------------------------------------------------------------- launches
+inline int entry_tiles(int w) { return w <= 16 ? 1 : w <= 32 ? 2 : w <= 64 ? 4 : 8; }
+inline long table_units(int S, long n_gh) { return n_gh * ssam_div_up(S, 32); }
+inline int table_slices(long units) { return (int)(units < 256 ? units : 256); }
+
+struct BwdWorkspace { size_t tab, gsum, stat, parts, total; };
+inline BwdWorkspace workspace_layout(int groups, int S, int w, int h, int d)
+{
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    const size_t rows = (size_t)groups * h * S, entries = rows * 32 * entry_tiles(w) * 2;
+    BwdWorkspace o;
+    o.tab = 0;
+    o.gsum = o.tab + up(entries);
+    o.stat = o.gsum + up(entries);
+    o.parts = o.stat + up(rows * 8);
+    o.total = o.parts + up((size_t)table_slices(table_units(S, (long)groups * h)) * 64 * entry_tiles(w) * d * 4);
+    return o;
+}
+
+template <typename Kernel>
+int allow_lds(Kernel k, size_t bytes)
+{
+    if (bytes > 160 * 1024) return SSAM_EUNSUPPORTED;
+    if (bytes > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return SSAM_EHIP;
+    return SSAM_OK;
+}
+
+template <int D, int NT>
+int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w, hipStream_t st)
+{
+    const int tiles = ssam_div_up(P.S, 128), nrel = 2 * P.w - 1;
+    const unsigned grid = (unsigned)((long)tiles * ssam_div_up(P.n_gh, 8) * 8);
+    const size_t lds = rows_lds_bytes<D, NT>(nrel);
+    if (int rc = allow_lds(attn_backward_rows_kernel<D, NT>, lds); rc != SSAM_OK) return rc;
+    if (int rc = allow_lds(attn_backward_columns_kernel<D, NT>, columns_lds_bytes<D, NT>()); rc != SSAM_OK) return rc;
+    hipLaunchKernelGGL((attn_backward_rows_kernel<D, NT>), dim3(grid), dim3(256), lds, st, P, tiles);
+    SSAM_CHECK_LAUNCH();
+    hipLaunchKernelGGL((attn_backward_columns_kernel<D, NT>), dim3(grid), dim3(256), (columns_lds_bytes<D, NT>()), st, P, tiles);
+    SSAM_CHECK_LAUNCH();
+    if (drel_h) {
+        const int per = ssam_div_up(P.S, 32), slices = table_slices(table_units(P.S, P.n_gh)), used = nrel * D;
+        hipLaunchKernelGGL((attn_backward_tables_kernel<D, NT>), dim3(slices), dim3(256), (tables_lds_bytes<D, NT>()), st, P, per, table_units(P.S, P.n_gh), parts);
+        SSAM_CHECK_LAUNCH();
+        hipLaunchKernelGGL(attn_backward_table_sums_kernel, dim3(ssam_div_up(used, 32), 2), dim3(256), 0, st, (const float4 *)parts, slices,
+                           2 * BwdCfg<D, NT>::WK * D, used, drel_h, drel_w);
+        SSAM_CHECK_LAUNCH();
+    }
+    return SSAM_OK;
+}
+
+template <int D>
+int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w, hipStream_t st)
+{
+    switch (entry_tiles(P.w)) {
+    case 1: return launch_backward<D, 1>(P, parts, drel_h, drel_w, st);
+    case 2: return launch_backward<D, 2>(P, parts, drel_h, drel_w, st);
+    case 4: return launch_backward<D, 4>(P, parts, drel_h, drel_w, st);
+    default: return launch_backward<D, 8>(P, parts, drel_h, drel_w, st);
+    }
+}
+
+bool backward_sizes_ok(int groups, int S, int w, int h, int d) { return groups > 0 && S > 0 && w > 0 && w <= 128 && h > 0 && d > 0 && (long)w * w == S; }
+
 }  // namespace
+
+extern "C" size_t ssam_sparse_attention_backward_workspace_bytes(int groups, int S, int w, int h, int d)
+{
+    return backward_sizes_ok(groups, S, w, h, d) ? workspace_layout(groups, S, w, h, d).total : 0;
+}
+
+extern "C" int ssam_sparse_attention_backward(const void *q, const void *k, const void *v, long row_stride, const void *rel_h, const void *rel_w,
+                                              const int32_t *sigma, long sigma_group_stride, const void *out, const void *dout, const int32_t *out_rows,
+                                              void *dq, void *dk, void *dv, long grad_stride, void *drel_h, void *drel_w,
+                                              int groups, int S, int w, int h, int d, int mask_block, double r, float scale,
+                                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q || !k || !v || !rel_h || !rel_w || !sigma || !out || !dout || !dq || !dk || !dv || !workspace || (!drel_h) != (!drel_w)) return SSAM_EINVAL;
+    if (groups <= 0 || S <= 0 || w <= 0 || h <= 0 || d <= 0 || !(r > 0.0) || r > 1.0 || !(scale > 0.f)) return SSAM_EINVAL;
+    if (sigma_group_stride != 0 && sigma_group_stride < S) return SSAM_EINVAL;
+    if ((long)w * w != S || row_stride < (long)h * d || row_stride % 8 != 0 || grad_stride < (long)h * d || grad_stride % 8 != 0) return SSAM_EINVAL;
+    for (const void *p : { q, k, v, rel_h, rel_w, out, dout, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)drel_h, (const void *)drel_w, (const void *)workspace })
+        if (!ssam_aligned16(p)) return SSAM_EINVAL;
+    if (mask_block == 32 ? S > 224 : mask_block != 128 || S > 16384) return SSAM_EUNSUPPORTED;
+    if (d != 16 && d != 32 && d != 64 && d != 80) return SSAM_EUNSUPPORTED;
+    if ((long)groups * h > 0x7ffffff0L || (long)ssam_div_up(S, 128) * ((long)groups * h + 7) > 0x7fffffffL / 256) return SSAM_EUNSUPPORTED;
+    const BwdWorkspace at = workspace_layout(groups, S, w, h, d);
+    if (workspace_bytes < at.total) return SSAM_EWORKSPACE;
+    unsigned char *ws = (unsigned char *)workspace;
+    BwdParams P;
+    P.q = (const bf16 *)q; P.k = (const bf16 *)k; P.v = (const bf16 *)v;
+    P.row_stride = row_stride;
+    P.rel_h = (const bf16 *)rel_h; P.rel_w = (const bf16 *)rel_w;
+    P.sigma = sigma;
+    P.sigma_stride = sigma_group_stride;
+    P.out = (const bf16 *)out; P.dout = (const bf16 *)dout;
+    P.out_rows = out_rows;
+    P.dq = (bf16 *)dq; P.dk = (bf16 *)dk; P.dv = (bf16 *)dv;
+    P.grad_stride = grad_stride;
+    P.S = S; P.w = w; P.h = h; P.n_gh = groups * h;
+    P.mask_block = mask_block;
+    P.n_pre = ssam_prefix_tiles(ssam_div_up(S, mask_block), r);
+    P.scale = scale;
+    P.scale_log2e = scale * LOG2E;
+    P.tab = (_Float16 *)(ws + at.tab);
+    P.gsum = drel_h ? (bf16 *)(ws + at.gsum) : nullptr;
+    P.stat = (float2 *)(ws + at.stat);
+    float *parts = (float *)(ws + at.parts);
+    hipStream_t st = (hipStream_t)stream;
+    switch (d) {
+    case 16: return launch_backward<16>(P, parts, (bf16 *)drel_h, (bf16 *)drel_w, st);
+    case 32: return launch_backward<32>(P, parts, (bf16 *)drel_h, (bf16 *)drel_w, st);
+    case 64: return launch_backward<64>(P, parts, (bf16 *)drel_h, (bf16 *)drel_w, st);
+    default: return launch_backward<80>(P, parts, (bf16 *)drel_h, (bf16 *)drel_w, st);
+    }
+}
