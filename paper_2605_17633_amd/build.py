@@ -52,11 +52,13 @@ def _resources(stderr: str):
 
 HOT = ("gemm_bf16_nt_", "gemm_ring_kernel", "gemm_direct_kernel", "gemm_wide_kernel", "attn_")     # kernels that are written to a register budget
 
+BACKWARD = ("backward_rows_kernel", "backward_columns_kernel", "backward_windows_kernel")                # likewise, of one wave to a SIMD with tables of 128 entries
+
 
 def spilled(kernels):
-    """Messages for the kernels of HOT that spill."""
+    """Messages for the kernels of HOT and BACKWARD that spill."""
     return [f"{k['name']}: {k['VGPRs Spill']} VGPRs spilled" for k in kernels
-            if k.get("VGPRs Spill", 0) > 0 and any(h in k["name"] for h in HOT)]
+            if k.get("VGPRs Spill", 0) > 0 and any(h in k["name"] for h in (*HOT, *BACKWARD))]
 
 
 def _compile(src: str, obj: str):

@@ -36,10 +36,15 @@ struct BwdParams {
     bf16 *dq, *dk, *dv;
     long grad_stride;
     int S, w, h, n_gh;
+    uint32_t per_w;              // 2^22 / w rounded up: a cell below 2^14 times it, over 2^22, is its row (the error, a cell / 2^22, is below 1 / w)
     int mask_block, n_pre;       // tile of the mask, tiles of the dense prefix
     float scale, scale_log2e, inv_scale, inv_scale_log2e;
     _Float16 *tab;               // [gh][SP][EW]: bias entries of a query, over the scale
     _Float16 *gsum;              // [gh][S][EW]: GH | GW over gunit; NULL: not wanted
+    // of every order (one, or one a group; see backward_prepare_kernel)
+    uint4 *e;                    // [order][SP][bytes of E]
+    uint32_t *blocks;            // [order][SP / 32]: the two slices of a block of keys, 0 if there are more
+    int32_t *inverse;            // [order][S]: position of a cell
     float *gunit;                // [gh][S]: a power of two
     float *lse, *delta;          // [gh][SP]: -log sum exp over the scale, -delta
     const uint4 *zeros;          // 1 KB of them
@@ -53,16 +58,21 @@ struct BwdCfg {
     static constexpr int KS = D / 16;                        // k-steps of a product over features
     static constexpr int ES = EW / 16;                       // and over entries
     static constexpr int DT = (D + 31) / 32;                 // 32-row tiles of dK^T, dV^T
-    static constexpr int CT = (D + EW + 31) / 32;            // and of [dQ | G]^T
-    static constexpr int KP = D + EW + 8, VP = D + 8;        // LDS pitches (elements): odd in 16-byte units
-    static constexpr int TP = EW + 8;                        // of bias entries
+    static constexpr int VP = D + 8;                         // LDS pitches (elements): odd in 16-byte units
     static constexpr int RP = 2 * WK + 8;                    // of G at relative positions, one table
-    static constexpr int ROW_KEYS = NT < 8 ? 64 : 32;        // keys of a stage of the row kernel
-    static constexpr bool KEEP = NT < 8;                     // a wave's queries, dO and bias entries stay in registers, else in LDS
+    static constexpr int UP = 4 * WK + 8;                    // of products with a table at the entries' places
 };
 
 // bit 23 of the mode register: fp16 results past the range are clamped instead of rounded to infinity (which would make NaNs of the zeros of E)
 __device__ __forceinline__ void clamp_fp16() { __builtin_amdgcn_s_setreg(1 | 23 << 6 | (1 - 1) << 11, 1); }
+
+// row | column << 16 of a position's cell (positions past the end: the last one's; cells are held to the grid)
+__device__ __forceinline__ int row_col(const int32_t *sigma, int at, const BwdParams &P)
+{
+    const int cell = min(max(sigma[min(at, P.S - 1)], 0), P.S - 1);
+    const int row = (int)((uint32_t)cell * P.per_w >> 22);
+    return row | (cell - row * P.w) << 16;
+}
 
 // MFMA passes done before results are read under predicates (see the forward kernels)
 __device__ __forceinline__ void mfma_settle()
@@ -129,201 +139,346 @@ __device__ __forceinline__ void store_rows(const f32x16 *acc, bf16 *scratch, bf1
     }
 }
 
+// Rows that go from memory straight into LDS lie there without padding; chunk c (16 bytes) of row r sits at place c ^ swizzle(r), so that 16 rows read at
+// one chunk touch all banks, and so do the 64 bytes each of 8 rows that a transposing read takes.
+template <int CHUNKS>
+__device__ __forceinline__ int swizzle(int row)
+{
+    if (CHUNKS >= 16) return (row & 1) << 3 | (row & 2) << 1 | (row & 4) >> 1 | (row & 8) >> 3;
+    if (CHUNKS == 8) return (row & 2) << 1 | (row & 4) >> 1 | (row & 8) >> 3;
+    if (CHUNKS == 4) return (row & 4) >> 1 | (row & 8) >> 3;
+    return (row >> 3) & 1;
+}
+
+// 16 bytes a lane from memory to LDS at lds + 16 * lane.  The compiler does not see the request: the caller waits for it (vmcnt).
+__device__ __forceinline__ void request(uint32_t lds, uint32_t off, const void *from)
+{
+    // (uniform, and kept in scalar registers: the compiler does not always do so for an operand of assembly)
+    const uint64_t f = reinterpret_cast<uint64_t>(from), base = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(f >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)f);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base) : "m0", "memory");
+}
+__device__ __forceinline__ void request(uint32_t lds, const void *src)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src) : "m0", "memory");
+}
+
+// Transposed operand of rows that lie so: columns 32 * tile + .. of 16 rows at `t`, in the order in which a 32x32 result holds them (operand a of step t).
+template <int CHUNKS>
+struct Transposed {
+    static constexpr int PITCH = CHUNKS * 16;
+    static constexpr int KINDS = CHUNKS == 8 ? 2 : 1;         // (rows of 16 chunks and more: the place of another tile is the first one's with bits changed)
+    int at[KINDS][2];
+    __device__ __forceinline__ Transposed()
+    {
+        const int lane = threadIdx.x & 63, li = lane & 15;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = 8 * u + 4 * (lane >> 5) + (li >> 2), f0 = (CHUNKS == 2 ? 0 : 16 * ((lane >> 4) & 1)) + 4 * (li & 3);
+#pragma unroll
+            for (int k = 0; k < KINDS; ++k) at[k][u] = r * PITCH + ((4 * k + (f0 >> 3)) ^ swizzle<CHUNKS>(r)) * 16 + (f0 & 7) * 2;
+        }
+    }
+    // base: byte offset of the block in LDS.  (Of a last tile that the rows fill by half, 10 chunks, the other half is the same columns again.)
+    __device__ __forceinline__ bf16x8 operator()(const unsigned char *smem, int base, int t, int tile) const
+    {
+        bf16x4 v[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            int a = CHUNKS >= 16 ? (at[0][u] ^ (tile & 3) * 64) + base + 16 * t * PITCH + tile / 4 * 256
+                                 : at[tile % KINDS][u] + base + 16 * t * PITCH + tile / KINDS * KINDS * 64;
+            if (CHUNKS == 10 && tile == 2) a -= ((threadIdx.x >> 4) & 1) * 32;
+            v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(smem + a));
+        }
+        return bf16x8{ v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3] };
+    }
+};
+
+// Operand a or b of step ks over features: 16 bytes of row l32 of a block.
+template <int CHUNKS>
+struct Straight {
+    static constexpr bool LINE = CHUNKS == 2 || CHUNKS == 10;   // the swizzle changes places by twos: those of a step are 32 bytes from the last one's
+    int at[LINE ? 1 : CHUNKS / 2];
+    __device__ __forceinline__ Straight()
+    {
+        const int lane = threadIdx.x & 63, l32 = lane & 31;
+#pragma unroll
+        for (int ks = 0; ks < (LINE ? 1 : CHUNKS / 2); ++ks) at[ks] = l32 * CHUNKS * 16 + ((2 * ks + (lane >> 5)) ^ swizzle<CHUNKS>(l32)) * 16;
+    }
+    __device__ __forceinline__ bf16x8 operator()(const unsigned char *smem, int base, int ks) const
+    {
+        return *reinterpret_cast<const bf16x8 *>(smem + base + (LINE ? at[0] + 32 * ks : at[LINE ? 0 : ks]));
+    }
+};
+
+// entries of a slice of 16, the eight of a half-wave: a one (of fp16) at place i, if that is one of them
+__device__ __forceinline__ f16x8 ones(int i)
+{
+    u32x4 e;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = i >> 1 == j ? (i & 1 ? 0x3c000000u : 0x3c00u) : 0u;
+    return __builtin_bit_cast(f16x8, e);
+}
+
+// ---------------------------------------------------------------- what the order alone decides
+// E of every key as the row kernel's stages take it, the slices of a block of 32 keys (row | column << 8 | 1 << 16, or 0), the inverse of the order.  A wave a block.
+template <int NT, bool LOCAL>
+__global__ void __launch_bounds__(256)
+backward_prepare_kernel(BwdParams P, int blocks, int total)
+{
+    constexpr int WK = 16 * NT, EC = LOCAL ? 4 : 4 * NT;
+    const int unit = (int)blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    if (blockIdx.x == 0 && threadIdx.x < 64) const_cast<uint4 *>(P.zeros)[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    if (unit >= total) return;
+    const int order = unit / blocks, at = (unit - order * blocks) * 32 + l32;
+    const int rc = row_col(P.sigma + (long)order * P.sigma_stride, at, P), row = rc & 0xffff, col = rc >> 16;
+    uint4 *to = P.e + ((long)order * P.SP + at) * EC;
+    if constexpr (LOCAL) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) to[2 * half + c] = __builtin_bit_cast(uint4, ones(((half ? col : row) & 15) - 8 * c));
+    } else {
+#pragma unroll
+        for (int c = 0; c < EC / 2; ++c) to[half * EC / 2 + c] = __builtin_bit_cast(uint4, ones((half ? col : row) - 8 * c));
+    }
+    static_assert(LOCAL || EC / 2 * 8 == WK, "");
+    const int rs = __builtin_amdgcn_readfirstlane(row >> 4), cs = __builtin_amdgcn_readfirstlane(col >> 4);
+    const bool two = __builtin_amdgcn_ballot_w64(row >> 4 != rs || col >> 4 != cs) == 0;
+    if (lane == 0) P.blocks[unit] = two ? (uint32_t)rs | (uint32_t)cs << 8 | 1u << 16 : 0u;
+    if (half == 0 && at < P.S) P.inverse[(long)order * P.S + row * P.w + col] = at;
+}
+
 // ---------------------------------------------------------------- rows
-template <int D, int NT>
+// Stages of a row walk, two buffers of them in LDS: K, V and E, straight from memory.
+// LOCAL: of a key E holds the one of its row's slice of 16 entries and that of its column's, 64 keys a stage.  A block of 32 keys whose cells lie in one slice each
+// (every one of the position-only order on a grid of a power of two) takes two bias products and one G product; in others every slice that occurs takes one, the other keys
+// masked.  Otherwise E is whole, 32 keys a stage, and all entries are multiplied: for orders that scatter a block's cells over the grid.
+template <int D, int NT, bool LOCAL>
+struct RowStage {
+    using C = BwdCfg<D, NT>;
+    static constexpr int KEYS = LOCAL ? 64 : 32;
+    static constexpr int KP = D * 2, EP = LOCAL ? 64 : C::EW * 2, TP = C::EW * 2;   // rows, in bytes
+    static constexpr int K = 0, V = K + KEYS * KP, E = V + KEYS * KP, BYTES = E + KEYS * EP;
+    static constexpr int T = 2 * BYTES, O = T + 4 * 32 * TP;
+    static constexpr bool KEEP = NT < 8;                      // a wave's dO stays in registers, else in LDS
+    static constexpr int TOTAL = O + (KEEP ? 0 : 4 * 32 * C::VP * 2);
+    static_assert(2 * BYTES <= 64 * 1024, "requests reach the first 64 KB");
+};
+
+template <int D, int NT, bool LOCAL>
 __host__ __device__ constexpr size_t rows_lds_bytes(int nrel)
 {
     using C = BwdCfg<D, NT>;
-    const size_t tables = (size_t)4 * 32 * C::TP * 2;
-    const size_t stage = (size_t)C::ROW_KEYS * (C::KP + C::VP) * 2 + tables + 16 + (C::KEEP ? 0 : (size_t)4 * 32 * 2 * C::VP * 2);
-    const size_t end = (size_t)4 * 32 * C::RP * 2 + (size_t)(nrel + 15) / 16 * 16 * C::VP * 2;
+    const size_t stage = RowStage<D, NT, LOCAL>::TOTAL, products = (size_t)4 * 32 * C::UP * 2;
+    const size_t end = (size_t)C::WK * 2 + (size_t)4 * 32 * C::RP * 2 + (size_t)(nrel + 15) / 16 * 16 * C::VP * 2;
     const size_t rows = (size_t)4 * 32 * C::VP * 2;
-    const size_t m = end > stage ? end : stage;
+    size_t m = end > stage ? end : stage;
+    m = products > m ? products : m;
     return rows > m ? rows : m;
 }
 
-template <int D, int NT>
+template <int D, int NT, bool LOCAL>
 __global__ void __launch_bounds__(256, NT < 8 ? 2 : 1)
-attn_backward_rows_kernel(BwdParams P, int tiles)
+backward_rows_kernel(BwdParams P, int tiles)
 {
     using C = BwdCfg<D, NT>;
+    using St = RowStage<D, NT, LOCAL>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
     // the tiles of one (group, head) run on one XCD (workgroup b sits on XCD b & 7), whose L2 then serves the re-reads of its K and V
     const int tile = (blockIdx.x >> 3) % tiles, gh = ((blockIdx.x >> 3) / tiles) * 8 + (blockIdx.x & 7);
     if (gh >= P.n_gh) return;
     clamp_fp16();
-    if (blockIdx.x == 0 && tid < 64) const_cast<uint4 *>(P.zeros)[tid] = make_uint4(0, 0, 0, 0);
     const int grp = gh / P.h, head = gh - grp * P.h;
     const int S = P.S, w = P.w, nrel = 2 * w - 1;
     const int q0 = tile * 128, qpos = q0 + wave * 32 + l32;
+    const int order = P.sigma_stride ? grp : 0;
     const int32_t *sigma = P.sigma + (long)grp * P.sigma_stride;
 
     // this lane's query: its features, dO and delta
     bf16x8 qf[C::KS], of[C::KS];
     float delta = 0.f;
-    int orow = -1, qrc = 0;                                  // row | column << 16 of the query's cell
-    if (qpos < S) {
-        const long slot = (long)grp * S + qpos;
-        const int cell = sigma[qpos];
-        qrc = cell / w;
-        qrc |= (cell - qrc * w) << 16;
-        orow = P.out_rows ? P.out_rows[slot] : 0;
-        const long at = (P.out_rows ? (long)orow : slot) * ((long)P.h * D) + (long)head * D + half * 8;
-        if (orow >= 0) {
-            const bf16 *qp = P.q + slot * P.row_stride + (long)head * D + half * 8;
+    int qrc = 0;                                             // row | column << 16 of the query's cell
+    {
+        int orow = -1;
+        if (qpos < S) {
+            const long slot = (long)grp * S + qpos;
+            qrc = row_col(sigma, qpos, P);
+            orow = P.out_rows ? P.out_rows[slot] : 0;
+            const long at = (P.out_rows ? (long)orow : slot) * ((long)P.h * D) + (long)head * D + half * 8;
+            if (orow >= 0) {
+                const bf16 *qp = P.q + slot * P.row_stride + (long)head * D + half * 8;
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) {
-                qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
-                of[ks] = *reinterpret_cast<const bf16x8 *>(P.dout + at + ks * 16);
-                const bf16x8 o = *reinterpret_cast<const bf16x8 *>(P.out + at + ks * 16);
+                for (int ks = 0; ks < C::KS; ++ks) {
+                    qf[ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 16);
+                    of[ks] = *reinterpret_cast<const bf16x8 *>(P.dout + at + ks * 16);
+                    const bf16x8 o = *reinterpret_cast<const bf16x8 *>(P.out + at + ks * 16);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) delta = fmaf((float)of[ks][e], (float)o[e], delta);
+                    for (int e = 0; e < 8; ++e) delta = fmaf((float)of[ks][e], (float)o[e], delta);
+                }
             }
         }
-    }
-    if (orow < 0) {                                          // past the end, or its output is dropped: no gradient comes from it
+        if (orow < 0) {                                      // past the end, or its output is dropped: no gradient comes from it
 #pragma unroll
-        for (int ks = 0; ks < C::KS; ++ks)
+            for (int ks = 0; ks < C::KS; ++ks)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) qf[ks][e] = of[ks][e] = (bf16)0.f;
+                for (int e = 0; e < 8; ++e) qf[ks][e] = of[ks][e] = (bf16)0.f;
+        }
     }
     delta += __shfl_xor(delta, 32, 64);
 
-    // bias entries over the scale: rel Q^T, relative position t of the lane's query is its entry at_q + w - 1 - t
-    _Float16 *tq = reinterpret_cast<_Float16 *>(smem) + (wave * 32 + l32) * C::TP;
-    for (int p = w + half; p < C::WK; p += 2) tq[p] = tq[C::WK + p] = (_Float16)0.f;
-    for (int m0 = 0; m0 < nrel; m0 += 32)
+    // Bias entries over the scale: rel Q^T, relative position t of the lane's query is its entry at_q + w - 1 - t.  All of a product's are stored, those below 0 and from w on
+    // at places of their own in a row that is long enough (no predicates: a store behind one costs ten instructions), and the entries read back from where they lie for every query.
+    f16x8 bt[C::ES];
+    {
+        _Float16 *u_row = reinterpret_cast<_Float16 *>(smem) + (wave * 32 + l32) * C::UP;
+        constexpr int FIRST = 2 * C::WK;                     // the place of entry 0
 #pragma unroll
         for (int tab = 0; tab < 2; ++tab) {
-            const bf16 *rp = (tab ? P.rel_w : P.rel_h) + (long)min(m0 + l32, nrel - 1) * D + half * 8;
-            f32x16 u = zero16();
+            wave_lds_fence();
+            _Float16 *to = u_row + (FIRST + w - 1 + (tab ? qrc >> 16 : qrc & 0xffff) - 4 * half);
+            for (int m0 = 0; m0 < nrel; m0 += 32, to -= 32) {
+                const bf16 *rp = (tab ? P.rel_w : P.rel_h) + (long)min(m0 + l32, nrel - 1) * D + half * 8;
+                f32x16 u = zero16();
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(rp + ks * 16), qf[ks], u, 0, 0, 0);
-            mfma_settle();
-            const int p0 = (tab ? qrc >> 16 : qrc & 0xffff) + w - 1 - m0 - 4 * half;
+                for (int ks = 0; ks < C::KS; ++ks) u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(rp + ks * 16), qf[ks], u, 0, 0, 0);
+                mfma_settle();
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int p = p0 - 8 * (r >> 2) - (r & 3);
-                if ((unsigned)p < (unsigned)w) tq[tab * C::WK + p] = (_Float16)(u[r] * P.inv_scale);
+                for (int r = 0; r < 16; ++r) to[-8 * (r >> 2) - (r & 3)] = (_Float16)(u[r] * P.inv_scale);
+            }
+            wave_lds_fence();
+#pragma unroll
+            for (int c = 0; c < C::ES / 2; ++c) {            // entries 16 c + 8 half .. + 7; those from w on are zeros
+                f16x8 v = *reinterpret_cast<const f16x8 *>(u_row + FIRST + 16 * c + 8 * half);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 16 * c + 8 * half + e < w ? v[e] : (_Float16)0.f;
+                bt[tab * C::ES / 2 + c] = v;
             }
         }
-    wave_lds_fence();
+    }
     if (qpos < P.SP) {
         _Float16 *to = P.tab + ((long)gh * P.SP + qpos) * C::EW + 8 * half;
 #pragma unroll
-        for (int c = 0; c < C::ES; ++c) *reinterpret_cast<f16x8 *>(to + 16 * c) = *reinterpret_cast<const f16x8 *>(tq + 16 * c + 8 * half);
+        for (int c = 0; c < C::ES; ++c) *reinterpret_cast<f16x8 *>(to + 16 * c) = bt[c];
     }
-    const _Float16 *tl = tq + 8 * half;
+    __syncthreads();
+    const int tsw = swizzle<C::EW / 8>(l32);
+    unsigned char *tl = smem + St::T + (wave * 32 + l32) * St::TP;
+#pragma unroll
+    for (int c = 0; c < C::ES; ++c) *reinterpret_cast<f16x8 *>(tl + ((2 * c + half) ^ tsw) * 16) = bt[c];
+
+    bf16 *os = reinterpret_cast<bf16 *>(smem + St::O) + (wave * 32 + l32) * C::VP + half * 8;
+    if constexpr (!St::KEEP)
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks) *reinterpret_cast<bf16x8 *>(os + ks * 16) = of[ks];
+    auto upstream = [&](int ks) { return St::KEEP ? of[ks] : *reinterpret_cast<const bf16x8 *>(os + ks * 16); };
 
     // stages of keys: the dense prefix, then (where a wave has a diagonal tile behind it) the workgroup's own 128
-    bf16 *Ks = reinterpret_cast<bf16 *>(smem) + 4 * 32 * (C::TP + (C::KEEP ? 0 : 2 * C::VP)), *Vs = Ks + C::ROW_KEYS * C::KP;
-    uint32_t *slices = reinterpret_cast<uint32_t *>(Vs + C::ROW_KEYS * C::VP);
-    // where registers are short, the wave's queries and dO lie behind the bias entries
-    bf16 *qs = reinterpret_cast<bf16 *>(smem) + 4 * 32 * C::TP + (wave * 32 + l32) * 2 * C::VP + half * 8, *os = qs + C::VP;
-    if constexpr (!C::KEEP)
-#pragma unroll
-        for (int ks = 0; ks < C::KS; ++ks) {
-            *reinterpret_cast<bf16x8 *>(qs + ks * 16) = qf[ks];
-            *reinterpret_cast<bf16x8 *>(os + ks * 16) = of[ks];
-        }
-    auto query = [&](int ks) { return C::KEEP ? qf[ks] : *reinterpret_cast<const bf16x8 *>(qs + ks * 16); };
-    auto upstream = [&](int ks) { return C::KEEP ? of[ks] : *reinterpret_cast<const bf16x8 *>(os + ks * 16); };
-    const int pre = min(P.n_pre * P.mask_block, S), pre_stages = (pre + C::ROW_KEYS - 1) / C::ROW_KEYS;
+    const int pre = min(P.n_pre * P.mask_block, S), pre_stages = (pre + St::KEYS - 1) / St::KEYS;
     const int own = (q0 + wave * 32) / P.mask_block;                                  // mask tile of the wave's queries
     const bool any_diagonal = min(q0 + 127, S - 1) / P.mask_block >= P.n_pre;
-    const int stages = pre_stages + (any_diagonal ? (min(128, S - q0) + C::ROW_KEYS - 1) / C::ROW_KEYS : 0);
+    const int stages = pre_stages + (any_diagonal ? (min(128, S - q0) + St::KEYS - 1) / St::KEYS : 0);
     const bool alive = q0 + wave * 32 < S;
+    auto stage_key = [&](int s) { return s < pre_stages ? s * St::KEYS : q0 + (s - pre_stages) * St::KEYS; };
 
-    for (int i = tid; i < C::ROW_KEYS * (C::EW / 8); i += 256)                       // E starts empty
-        *reinterpret_cast<uint4 *>(Ks + (i / (C::EW / 8)) * C::KP + D + (i % (C::EW / 8)) * 8) = make_uint4(0, 0, 0, 0);
-
-    // Places of a thread's chunks are worked out again at every stage (`fresh`): kept, they would take registers from the accumulators.
-    auto fresh = [&]() { int t = tid; asm volatile("" : "+v"(t)); return t; };
-    constexpr int CH = D / 8, SIDE = C::ROW_KEYS * CH, NLOAD = (SIDE + 255) / 256;
-    u32x4 kr[NLOAD], vr[NLOAD];
-    int cell_next = -1;
+    constexpr int CH = D / 8, NI = St::KEYS * CH / 64, NQ = (NI + 3) / 4, EC = St::EP / 16, EI = St::KEYS * EC / 64, NE = (EI + 3) / 4;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)smem);
     const bf16 *kbase = P.k + (long)grp * S * P.row_stride + (long)head * D, *vbase = P.v + (long)grp * S * P.row_stride + (long)head * D;
-    auto stage_key = [&](int s) { return s < pre_stages ? s * C::ROW_KEYS : q0 + (s - pre_stages) * C::ROW_KEYS; };
+    const uint4 *ebase = P.e + (long)order * P.SP * EC;
     auto load = [&](int s) {
-        const int key0 = stage_key(s), t = fresh();
+        int ln = lane;
+        if (D == 80) asm volatile("" : "+v"(ln));            // places are worked out again at every stage: kept, they would take registers that are short
+        const int key0 = stage_key(s);
+        const uint32_t to = lds0 + (s & 1) * St::BYTES;
+        const unsigned char *ks = reinterpret_cast<const unsigned char *>(kbase) + (long)key0 * P.row_stride * 2, *vs = reinterpret_cast<const unsigned char *>(vbase) + (long)key0 * P.row_stride * 2;
 #pragma unroll
-        for (int i = 0; i < NLOAD; ++i) {
-            const int id = t + 256 * i, row = id / CH, c = id - row * CH;
-            kr[i] = vr[i] = u32x4{ 0, 0, 0, 0 };
-            if (id < SIDE && key0 + row < S) {               // (a group's rows lie within 2^31 bytes)
-                const uint32_t at = (uint32_t)(key0 + row) * (uint32_t)P.row_stride + c * 8;
-                kr[i] = *reinterpret_cast<const u32x4 *>(kbase + at);
-                vr[i] = *reinterpret_cast<const u32x4 *>(vbase + at);
+        for (int i = 0; i < NQ; ++i) {
+            const int j = wave + 4 * i;
+            if (j >= NI) continue;
+            const int at = j * 64 + ln, r = at / CH, c = at % CH ^ swizzle<CH>(r);
+            const uint32_t off = r * (uint32_t)P.row_stride * 2 + c * 16;
+            if (key0 + St::KEYS <= S) {
+                request(to + St::K + j * 1024, off, ks);
+                request(to + St::V + j * 1024, off, vs);
+            } else {                                         // keys past the end are zeros
+                const bool in = key0 + r < S;
+                request(to + St::K + j * 1024, in ? ks + off : (const void *)P.zeros);
+                request(to + St::V + j * 1024, in ? vs + off : (const void *)P.zeros);
             }
         }
-        if (tid < C::ROW_KEYS) cell_next = key0 + tid < S ? sigma[key0 + tid] : -1;
-    };
-    int ones = -1;                                           // where this thread's key has its ones: row | column << 8
-    auto store = [&]() {
-        const int t = fresh();
+        // (rows of E from SP on are another order's, or what follows them: blocks past the end are left out)
 #pragma unroll
-        for (int i = 0; i < NLOAD; ++i) {
-            const int id = t + 256 * i, row = id / CH, c = id - row * CH;
-            if (id < SIDE) {
-                *reinterpret_cast<u32x4 *>(Ks + row * C::KP + c * 8) = kr[i];
-                *reinterpret_cast<u32x4 *>(Vs + row * C::VP + c * 8) = vr[i];
-            }
-        }
-        if (wave == 0 && tid < C::ROW_KEYS) {
-            uint16_t *e = reinterpret_cast<uint16_t *>(Ks + tid * C::KP + D);
-            if (ones >= 0) e[ones & 0xff] = e[ones >> 8] = 0;
-            ones = -1;
-            if (cell_next >= 0) {
-                const int row = cell_next / w, col = C::WK + cell_next - row * w;
-                ones = row | col << 8;
-                e[row] = e[col] = 0x3c00;
-            }
-            // slices of 16 entries: where all keys of a block have their ones in the same two (rows and columns), the others are left out
-            const int s2 = ones >> 4 & 0xf0f, first = __shfl(s2, lane & 32, 64);
-            const uint64_t differ = __builtin_amdgcn_ballot_w64(ones >= 0 && s2 != first);
-            if ((lane & 31) == 0) slices[lane >> 5] = (uint32_t)(differ >> (lane & 32)) == 0 ? (uint32_t)s2 | 0x10000u : 0u;
+        for (int i = 0; i < NE; ++i) {
+            const int j = wave + 4 * i;
+            if (j >= EI) continue;
+            const int at = j * 64 + ln, r = at / EC, c = at % EC ^ swizzle<EC>(r);
+            request(to + St::E + j * 1024, (uint32_t)(r * EC + c) * 16, ebase + (long)key0 * EC);
         }
     };
+    const uint32_t *blocks = P.blocks + (long)order * (P.SP / 32);
 
-    f32x16 acc[C::CT];
+    const Transposed<CH> kt;
+    const Transposed<EC> et;
+    const Straight<CH> ka;
+    const int esw = swizzle<EC>(l32);
+
+    f32x16 acc[C::DT], gt[LOCAL ? 1 : NT];
+    float g[LOCAL ? C::ES : 1][8];
 #pragma unroll
-    for (int t = 0; t < C::CT; ++t) acc[t] = zero16();
-    asm volatile("" : "+v"(qrc));
+    for (int t = 0; t < C::DT; ++t) acc[t] = zero16();
+#pragma unroll
+    for (int t = 0; t < (LOCAL ? 1 : NT); ++t) gt[t] = zero16();
+#pragma unroll
+    for (int s = 0; s < (LOCAL ? C::ES : 1); ++s)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) g[s][r] = 0.f;
     float m = -INFINITY, l = 0.f;
     __syncthreads();
-    if (stages > 0) load(0);
+    load(0);
     for (int s = 0; s < stages; ++s) {
-        LDS_BARRIER();                                       // every wave is done with the previous stage
-        store();
-        LDS_BARRIER();
-        const int key0 = stage_key(s);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        LDS_BARRIER();                                       // this stage has landed, and nobody reads the other buffers any more
         if (s + 1 < stages) load(s + 1);
+        const int key0 = stage_key(s);
 #pragma unroll 1
-        for (int b = 0; b < C::ROW_KEYS / 32; ++b) {
+        for (int b = 0; b < St::KEYS / 32; ++b) {
             const int kb = key0 + 32 * b;
             const bool active = alive && kb < S && (s < pre_stages ? kb < pre : own >= P.n_pre && kb / P.mask_block == own);
             if (!active) continue;                           // the same for the whole wave
-            const bf16 *kblk = Ks + 32 * b * C::KP, *vblk = Vs + 32 * b * C::VP;
-            const bf16 *kl = kblk + l32 * C::KP + half * 8, *vl = vblk + l32 * C::VP + half * 8;
-            const uint32_t two = NT > 1 ? __builtin_amdgcn_readfirstlane(slices[b]) : 0;
-            const int rs = two & 0xff, cs = (two >> 8) & 0xff;
+            const int at = (s & 1) * St::BYTES + 32 * b * St::KP, eat = (s & 1) * St::BYTES + St::E + 32 * b * St::EP;
+            const unsigned char *el = smem + eat + l32 * St::EP;
             f32x16 sc = zero16();
-            if (NT > 1 && two != 0) {
-                sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(kl + D + rs * 16), *reinterpret_cast<const f16x8 *>(tl + 16 * rs), sc, 0, 0, 0);
-                sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(kl + D + cs * 16), *reinterpret_cast<const f16x8 *>(tl + 16 * cs), sc, 0, 0, 0);
+            int rs = 0, cs = 0, rc = 0;
+            bool two = true;
+            if constexpr (LOCAL && C::ES > 2) {
+                const uint32_t slices = __builtin_amdgcn_readfirstlane(blocks[kb >> 5]);
+                two = slices != 0;
+                rs = slices & 0xff;
+                cs = slices >> 8 & 0xff;
+                if (!two) rc = row_col(sigma, kb + l32, P);
+            }
+            if constexpr (LOCAL) {
+                const f16x8 er = *reinterpret_cast<const f16x8 *>(el + (half ^ esw) * 16), ec = *reinterpret_cast<const f16x8 *>(el + ((2 + half) ^ esw) * 16);
+                if (two) {
+                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(er, *reinterpret_cast<const f16x8 *>(tl + ((2 * rs + half) ^ tsw) * 16), sc, 0, 0, 0);
+                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ec, *reinterpret_cast<const f16x8 *>(tl + ((2 * cs + C::WK / 8 + half) ^ tsw) * 16), sc, 0, 0, 0);
+                } else {
+                    const f16x8 none = { 0, 0, 0, 0, 0, 0, 0, 0 };
+#pragma unroll 1
+                    for (int i = 0; i < C::ES; ++i) {
+                        const bool is_row = i < C::ES / 2, mine = (is_row ? rc >> 4 & 15 : (rc >> 20) + C::ES / 2) == i;
+                        if (__builtin_amdgcn_ballot_w64(mine) == 0) continue;
+                        sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(mine ? (is_row ? er : ec) : none, *reinterpret_cast<const f16x8 *>(tl + ((2 * i + half) ^ tsw) * 16), sc, 0, 0, 0);
+                    }
+                }
             } else {
 #pragma unroll
-                for (int c = 0; c < C::ES; ++c) {
-                    if (!C::KEEP && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(kl + D + c * 16), *reinterpret_cast<const f16x8 *>(tl + 16 * c), sc, 0, 0, 0);
-                }
+                for (int c = 0; c < C::ES; ++c)
+                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(el + ((2 * c + half) ^ esw) * 16), *reinterpret_cast<const f16x8 *>(tl + ((2 * c + half) ^ tsw) * 16), sc, 0, 0, 0);
             }
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(kl + ks * 16), query(ks), sc, 0, 0, 0);
+            for (int ks = 0; ks < C::KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka(smem, at + St::K, ks), qf[ks], sc, 0, 0, 0);
             f32x16 dp = zero16();
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(vl + ks * 16), upstream(ks), dp, 0, 0, 0);
+            for (int ks = 0; ks < C::KS; ++ks) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka(smem, at + St::V, ks), upstream(ks), dp, 0, 0, 0);
             float mx = -INFINITY;
             if (kb + 32 > S)
 #pragma unroll
@@ -338,10 +493,19 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
                 m = to;
                 l *= alpha;
 #pragma unroll
-                for (int t = 0; t < C::CT; ++t) {
-                    if (!C::KEEP) __builtin_amdgcn_sched_barrier(0);
+                for (int t = 0; t < C::DT; ++t)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[t][r] *= alpha;
+                if constexpr (LOCAL && C::ES > 2) {
+#pragma unroll
+                    for (int i = 0; i < C::ES; ++i)
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) g[i][r] *= alpha;
+                } else {
+#pragma unroll
+                    for (int t = 0; t < (LOCAL ? 1 : NT); ++t)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) gt[t][r] *= alpha;
                 }
             }
 #pragma unroll
@@ -354,11 +518,40 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int c = 0; c < C::CT; ++c) {
-                    // eleven tiles of accumulators leave no registers for operands read further ahead
-                    if (!C::KEEP && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(kblk, C::KP, t, c, D + C::EW - 4), ds[t], acc[c], 0, 0, 0);
+                for (int c = 0; c < C::DT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt(smem, at + St::K, t, c), ds[t], acc[c], 0, 0, 0);
+            if constexpr (!LOCAL) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) gt[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, t, c), ds[t], gt[c], 0, 0, 0);
+            } else if constexpr (C::ES == 2) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) gt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, t, 0), ds[t], gt[0], 0, 0, 0);
+            } else {
+                // rows' slice in registers 0 to 7 of the product, columns' in 8 to 15
+#pragma unroll 1
+                for (int i = 0; i < (two ? 1 : C::ES); ++i) {
+                    bf16x8 some[2] = { ds[0], ds[1] };
+                    int to_r = rs, to_c = cs + C::ES / 2;
+                    if (!two) {                              // dS of the keys in slice i
+                        const bool is_row = i < C::ES / 2;
+                        const uint32_t keys = (uint32_t)__builtin_amdgcn_ballot_w64((is_row ? rc >> 4 & 15 : (rc >> 20) + C::ES / 2) == i);
+                        if (keys == 0) continue;
+                        to_r = is_row ? i : -1;
+                        to_c = is_row ? -1 : i;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) some[r >> 3][r & 7] = keys >> (8 * (r >> 2) + (r & 3) + 4 * half) & 1 ? ds[r >> 3][r & 7] : (bf16)0.f;
+                    }
+                    f32x16 part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, 0, 0), some[0], zero16(), 0, 0, 0);
+                    part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, 1, 0), some[1], part, 0, 0, 0);
+                    mfma_settle();
+#pragma unroll
+                    for (int k = 0; k < C::ES; ++k)
+                        if (k == (k < C::ES / 2 ? to_r : to_c))
+#pragma unroll
+                            for (int r = 0; r < 8; ++r) g[k][r] += part[(k < C::ES / 2 ? 0 : 8) + r];
                 }
+            }
         }
     }
     mfma_settle();
@@ -371,22 +564,23 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
     const float inv = 1.f / l;
     float most = 0.f;
 #pragma unroll
-    for (int c = 0; c < C::CT; ++c) {
-        if (!C::KEEP) __builtin_amdgcn_sched_barrier(0);
+    for (int c = 0; c < C::DT; ++c)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const bool is_g = c * 32 + 8 * g >= D;                                    // (a group of eight columns is on one side)
-            const float f = is_g ? inv * 128.f : inv * P.scale;
+        for (int r = 0; r < 16; ++r) acc[c][r] = alive ? acc[c][r] * (inv * P.scale) : 0.f;
+    // G of slice i: register r <-> entry 16 i + 8 (r >> 2) + 4 half + (r & 3)
+    auto gs = [&](int i, int r) -> float { return LOCAL && C::ES > 2 ? g[LOCAL ? i : 0][r] : gt[LOCAL ? 0 : i >> 1][(i & 1) * 8 + r]; };
+    auto set_gs = [&](int i, int r, float v) { if constexpr (LOCAL && C::ES > 2) g[i][r] = v; else gt[LOCAL ? 0 : i >> 1][(i & 1) * 8 + r] = v; };
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float v = alive ? acc[c][4 * g + e] * f : 0.f;
-                acc[c][4 * g + e] = v;
-                if (is_g && c * 32 + 8 * g < D + C::EW) most = fmaxf(most, fabsf(v));
-            }
+    for (int i = 0; i < C::ES; ++i)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            const float v = alive ? gs(i, r) * (inv * 128.f) : 0.f;
+            set_gs(i, r, v);
+            most = fmaxf(most, fabsf(v));
         }
-    }
 
-    bf16 *gr = reinterpret_cast<bf16 *>(smem) + wave * 32 * C::RP, *rel = reinterpret_cast<bf16 *>(smem) + 4 * 32 * C::RP;
+    // (in front of the first row WK places that entries from w on, zeros, may go to)
+    bf16 *gr = reinterpret_cast<bf16 *>(smem) + C::WK + wave * 32 * C::RP, *rel = reinterpret_cast<bf16 *>(smem) + C::WK + 4 * 32 * C::RP;
     bf16 *mine = gr + l32 * C::RP;
     const int relrows = (nrel + 15) / 16 * 16;
     __syncthreads();
@@ -396,13 +590,11 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 127);
         const float unit = __uint_as_float((uint32_t)(e - 14 + 127) << 23), over = __uint_as_float((uint32_t)(14 - e + 127) << 23);
 #pragma unroll
-        for (int c = 0; c < C::CT; ++c)
+        for (int i = 0; i < C::ES; ++i)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = c * 32 + 8 * g - D;
-                if (col < 0 || col >= C::EW) continue;
-                f16x4 v = { (_Float16)(acc[c][4 * g] * over), (_Float16)(acc[c][4 * g + 1] * over), (_Float16)(acc[c][4 * g + 2] * over), (_Float16)(acc[c][4 * g + 3] * over) };
-                *reinterpret_cast<f16x4 *>(mine + col + 4 * half) = v;
+            for (int k = 0; k < 2; ++k) {
+                const f16x4 v = { (_Float16)(gs(i, 4 * k) * over), (_Float16)(gs(i, 4 * k + 1) * over), (_Float16)(gs(i, 4 * k + 2) * over), (_Float16)(gs(i, 4 * k + 3) * over) };
+                *reinterpret_cast<f16x4 *>(mine + 16 * i + 8 * k + 4 * half) = v;
             }
         if (qpos < S && half == 0) P.gunit[(long)gh * S + qpos] = unit;
         wave_lds_fence();
@@ -425,21 +617,18 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
         }
         for (int i = 8 * half; i < relrows; i += 16) *reinterpret_cast<uint4 *>(mine + i) = make_uint4(0, 0, 0, 0);
         const int t0 = (tab ? qrc >> 16 : qrc & 0xffff) + w - 1;
-        f32x16 add[C::DT];
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt) add[dt] = zero16();
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             wave_lds_fence();
 #pragma unroll
-            for (int c = 0; c < C::CT; ++c)
+            for (int i = tab * C::ES / 2; i < (tab + 1) * C::ES / 2; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (c * 32 + 8 * (r >> 2) < D + tab * C::WK || c * 32 + 8 * (r >> 2) >= D + (tab + 1) * C::WK) continue;
-                    const int y = c * 32 + 8 * (r >> 2) + (r & 3) + 4 * half - D - tab * C::WK;
-                    const bf16 v = (bf16)acc[c][r];
-                    if (y < w) mine[t0 - y] = v;
-                    if (part == 0) acc[c][r] -= (float)v;
+                for (int r = 0; r < 8; ++r) {
+                    const int y = 16 * (i - tab * C::ES / 2) + 8 * (r >> 2) + (r & 3);       // + 4 * half
+                    const float x = gs(i, r);
+                    const bf16 v = (bf16)x;
+                    mine[t0 - 4 * half - y] = v;             // (zeros of entries from w on: places of zeros, in front of the row the unused end of the one before)
+                    if (part == 0) set_gs(i, r, x - (float)v);
                 }
             if (part == 0) __syncthreads();
             else wave_lds_fence();
@@ -447,42 +636,16 @@ attn_backward_rows_kernel(BwdParams P, int tiles)
                 const bf16x4 a = *reinterpret_cast<const bf16x4 *>(mine + 16 * t + 4 * half), b = *reinterpret_cast<const bf16x4 *>(mine + 16 * t + 8 + 4 * half);
                 const bf16x8 g8 = { a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3] };
 #pragma unroll
-                for (int dt = 0; dt < C::DT; ++dt) add[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(rel + 16 * t * C::VP, C::VP, 0, dt, D - 4), g8, add[dt], 0, 0, 0);
+                for (int dt = 0; dt < C::DT; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(rel + 16 * t * C::VP, C::VP, 0, dt, D - 4), g8, acc[dt], 0, 0, 0);
             }
         }
         mfma_settle();
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (dt * 32 + 8 * (r >> 2) < D) acc[dt][r] += add[dt][r];             // (the rest of a last tile that D fills by half is GH)
     }
     __syncthreads();
     store_rows<D>(acc, reinterpret_cast<bf16 *>(smem) + wave * 32 * C::VP, P.dq + (long)grp * S * P.grad_stride + (long)head * D, P.grad_stride, qpos < S ? qpos : -1);
 }
 
 // ---------------------------------------------------------------- columns
-// Rows that go from memory straight into LDS lie there without padding; chunk c (16 bytes) of row r sits at place c ^ swizzle(r), so that 16 rows read at
-// one chunk touch all banks, and so do the 64 bytes each of 8 rows that a transposing read takes.
-template <int CHUNKS>
-__device__ __forceinline__ int swizzle(int row)
-{
-    if (CHUNKS >= 16) return (row & 1) << 3 | (row & 2) << 1 | (row & 4) >> 1 | (row & 8) >> 3;
-    if (CHUNKS == 8) return (row & 2) << 1 | (row & 4) >> 1 | (row & 8) >> 3;
-    if (CHUNKS == 4) return (row & 4) >> 1 | (row & 8) >> 3;
-    return (row >> 3) & 1;
-}
-
-// 16 bytes a lane from memory to LDS at lds + 16 * lane.  The compiler does not see the request: the caller waits for it (vmcnt).
-__device__ __forceinline__ void request(uint32_t lds, uint32_t off, const void *base)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(base) : "m0", "memory");
-}
-__device__ __forceinline__ void request(uint32_t lds, const void *src)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src) : "m0", "memory");
-}
-
 // Stages of a column walk, two buffers of them in LDS.  LOCAL: bias entries of the up to four slices (16 entries) that the workgroup's 128 keys have ones in
 // (all that there are up to 32 x 32; three on the position-only order of a 64 x 64 grid), 64 queries.  Otherwise of all slices, 32 queries.
 // Requests reach the first 64 KB of LDS.
@@ -522,12 +685,6 @@ __device__ __forceinline__ void walk_queries(const BwdParams &P, unsigned char *
     // slice in a slot: the wanted ones in order; a slot without one repeats the first, whose entries meet zeros of E
     uint32_t slices = 0;                                     // a byte each
     f16x8 ef[St::SLOTS];
-    auto ones = [&](int i) {                                 // entries of a slice: a one at place i, if that is one of its eight
-        u32x4 e;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = i >> 1 == j ? (i & 1 ? 0x3c000000u : 0x3c00u) : 0u;
-        return __builtin_bit_cast(f16x8, e);
-    };
     uint32_t left = wanted;
 #pragma unroll
     for (int s = 0; s < St::SLOTS; ++s) {
@@ -590,29 +747,9 @@ __device__ __forceinline__ void walk_queries(const BwdParams &P, unsigned char *
         if (wave == 3 && lane < 2 * FOURS) request(to + St::L, (lane < FOURS ? P.lse : P.delta) + (long)gh * P.SP + q0 + 4 * (lane % FOURS));
     };
 
-    // places of this lane's operands in a buffer: rows l32 of a block by 16-byte chunks, and transposed (rows +0 and +8)
-    int ka[C::KS], tr[CH == 8 ? 2 : 1][2];
-#pragma unroll
-    for (int ks = 0; ks < C::KS; ++ks) ka[ks] = l32 * St::QP + ((2 * ks + half) ^ swizzle<CH>(l32)) * 16;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int li = lane & 15, r = 8 * u + 4 * half + (li >> 2);
-#pragma unroll
-        for (int dt = 0; dt < (CH == 8 ? 2 : 1); ++dt) {
-            const int f0 = (D == 16 ? 0 : 16 * ((lane >> 4) & 1)) + 4 * (li & 3);
-            tr[dt][u] = r * St::QP + ((4 * dt + (f0 >> 3)) ^ swizzle<CH>(r)) * 16 + (f0 & 7) * 2;
-        }
-    }
-    auto transpose = [&](int base, int t, int dt) {
-        bf16x4 v[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            int at = tr[CH == 8 ? dt : 0][u] + base + 16 * t * St::QP + (CH == 8 ? 0 : dt * 64);
-            if (D == 80 && dt == 2) at -= ((lane >> 4) & 1) * 32;       // the other half of a last tile that D fills by half: the same columns, not used
-            v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(smem + at));
-        }
-        return bf16x8{ v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3] };
-    };
+    // places of this lane's operands in a buffer: rows l32 of a block by 16-byte chunks, and transposed
+    const Straight<CH> qa;
+    const Transposed<CH> qt;
 
     int buf = 0;
     if (first < last) stage(first, 0);
@@ -644,9 +781,9 @@ __device__ __forceinline__ void walk_queries(const BwdParams &P, unsigned char *
                 for (int s = 0; s < St::SLOTS; ++s) p = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(tl + (2 * s ^ sw) * 16), ef[s], p, 0, 0, 0);
             }
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(smem + at + St::Q + ka[ks]), kf[ks], p, 0, 0, 0);
+            for (int ks = 0; ks < C::KS; ++ks) p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qa(smem, at + St::Q, ks), kf[ks], p, 0, 0, 0);
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) ds = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(smem + at + St::O + ka[ks]), vf[ks], ds, 0, 0, 0);
+            for (int ks = 0; ks < C::KS; ++ks) ds = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qa(smem, at + St::O, ks), vf[ks], ds, 0, 0, 0);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 p[r] = __builtin_amdgcn_exp2f(p[r] * P.scale_log2e);
@@ -657,8 +794,8 @@ __device__ __forceinline__ void walk_queries(const BwdParams &P, unsigned char *
                 const bf16x8 pf = half_of(p, t), df = half_of(ds, t);
 #pragma unroll
                 for (int dt = 0; dt < C::DT; ++dt) {
-                    dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transpose(at + St::O, t, dt), pf, dv[dt], 0, 0, 0);
-                    dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transpose(at + St::Q, t, dt), df, dk[dt], 0, 0, 0);
+                    dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qt(smem, at + St::O, t, dt), pf, dv[dt], 0, 0, 0);
+                    dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qt(smem, at + St::Q, t, dt), df, dk[dt], 0, 0, 0);
                 }
             }
         }
@@ -667,7 +804,7 @@ __device__ __forceinline__ void walk_queries(const BwdParams &P, unsigned char *
 
 template <int D, int NT>
 __global__ void __launch_bounds__(256, NT < 8 ? 2 : 1)
-attn_backward_columns_kernel(BwdParams P, ColWork work, float *__restrict__ parts)
+backward_columns_kernel(BwdParams P, ColWork work, float *__restrict__ parts)
 {
     using C = BwdCfg<D, NT>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -687,7 +824,7 @@ attn_backward_columns_kernel(BwdParams P, ColWork work, float *__restrict__ part
     }
     if (gh >= P.n_gh) return;
     const int grp = gh / P.h, head = gh - grp * P.h;
-    const int S = P.S, w = P.w;
+    const int S = P.S;
     const int k0 = tile * 128, kb = k0 + wave * 32, kpos = kb + l32;
     const int at = min(kpos, S - 1);                         // keys past the end repeat the last one; their results are not stored
     bf16x8 kf[C::KS], vf[C::KS];
@@ -697,7 +834,7 @@ attn_backward_columns_kernel(BwdParams P, ColWork work, float *__restrict__ part
         kf[ks] = *reinterpret_cast<const bf16x8 *>(P.k + o + ks * 16);
         vf[ks] = *reinterpret_cast<const bf16x8 *>(P.v + o + ks * 16);
     }
-    const int cell = P.sigma[(long)grp * P.sigma_stride + at], row = cell / w, col = C::WK + cell - row * w;
+    const int rc = row_col(P.sigma + (long)grp * P.sigma_stride, at, P), row = rc & 0xffff, col = C::WK + (rc >> 16);
     const int rs = __builtin_amdgcn_readfirstlane(row >> 4), cs = __builtin_amdgcn_readfirstlane(col >> 4);
     const bool two = __builtin_amdgcn_ballot_w64(row >> 4 != rs || col >> 4 != cs) == 0;       // all of the wave's keys have their ones in the same two slices
     uint32_t wanted = (1u << C::ES) - 1;
@@ -754,7 +891,7 @@ attn_backward_columns_kernel(BwdParams P, ColWork work, float *__restrict__ part
 
 // dK and dV of the prefix's keys: the slices' sums.  A thread has eight columns of one of the two.
 __global__ void __launch_bounds__(256)
-attn_backward_join_kernel(BwdParams P, ColWork work, int D, const float4 *__restrict__ parts, long n)
+backward_join_kernel(BwdParams P, ColWork work, int D, const float4 *__restrict__ parts, long n)
 {
     const long i = (long)blockIdx.x * 256 + threadIdx.x;
     const int per = 2 * D / 8;
@@ -773,127 +910,146 @@ attn_backward_join_kernel(BwdParams P, ColWork work, int D, const float4 *__rest
 }
 
 // ---------------------------------------------------------------- tables
-// A unit is 32 queries of one (group, head).  A workgroup adds up those of a slice in registers: result [relative position of both tables][feature].
-template <int D, int NT>
-__host__ __device__ constexpr size_t tables_lds_bytes()
-{
-    using C = BwdCfg<D, NT>;
-    return (size_t)32 * (2 * (4 * C::WK + 8) + C::VP) * 2;
-}
+// drel_h[t] = sum over rows R of H_R[R + w - 1 - t], H_R[y] = sum over the queries i in row R of GH[i][y] q_i, in all groups and heads; drel_w likewise by columns.  H_R is a plain
+// product over queries, with nothing to shift.  A workgroup has one R of one table and a slice of the (group, head); 64 queries a step, G as the sum of two bf16.
+constexpr int TABLE_QUERIES = 64;
 
 template <int D, int NT>
-__global__ void __launch_bounds__(256, NT >= 8 ? 1 : 2)
-attn_backward_tables_kernel(BwdParams P, int units_per_gh, long units, float *__restrict__ parts)
+struct TableStage {
+    using C = BwdCfg<D, NT>;
+    static constexpr int GP = C::WK + 8;                      // odd in 16-byte units (C::VP too)
+    static constexpr int MT = (C::WK + 31) / 32;              // 32-row tiles of entries
+    static constexpr int TILES = MT * C::DT, MINE = (TILES + 3) / 4;
+    static constexpr size_t BYTES = (size_t)TABLE_QUERIES * (2 * GP + C::VP) * 2;
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(256)
+backward_tables_kernel(BwdParams P, int slices, float *__restrict__ parts)
 {
     using C = BwdCfg<D, NT>;
-    constexpr int TT = 4 * C::WK / 32;                       // 32-row tiles of relative positions
-    constexpr int MINE = (TT + 3) / 4, GP = 4 * C::WK + 8;
+    using St = TableStage<D, NT>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    bf16 *Gs = reinterpret_cast<bf16 *>(smem), *Qs = Gs + 2 * 32 * GP;       // G is the sum of two bf16, one [32][GP] behind the other
+    bf16 *hi = reinterpret_cast<bf16 *>(smem), *lo = hi + TABLE_QUERIES * St::GP, *Qs = lo + TABLE_QUERIES * St::GP;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
-    const int S = P.S, w = P.w;
-    f32x16 acc[MINE][C::DT];
+    const int w = P.w, S = P.S;
+    const int tab = blockIdx.x / (w * slices), R = blockIdx.x / slices % w, slice = blockIdx.x % slices;
+    const long all = (long)P.n_gh * w, per = (all + slices - 1) / slices, last = min((slice + 1) * per, all);
+    f32x16 acc[St::MINE];
 #pragma unroll
-    for (int i = 0; i < MINE; ++i)
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt) acc[i][dt] = zero16();
-    const long per = (units + gridDim.x - 1) / gridDim.x, u1 = min((long)(blockIdx.x + 1) * per, units);
-    for (long u = blockIdx.x * per; u < u1; ++u) {
-        const int gh = (int)(u / units_per_gh), q0 = (int)(u - (long)gh * units_per_gh) * 32, grp = gh / P.h, head = gh - grp * P.h;
+    for (int i = 0; i < St::MINE; ++i) acc[i] = zero16();
+    constexpr int CH = D / 8, GC = C::WK / 8;
+    static_assert(TABLE_QUERIES * GC % 128 == 0, "");
+    for (long k0 = slice * per; k0 < last; k0 += TABLE_QUERIES) {
         __syncthreads();
-        for (int i = tid; i < 2 * 32 * (GP / 8); i += 256) *reinterpret_cast<uint4 *>(Gs + i * 8) = make_uint4(0, 0, 0, 0);
-        constexpr int CH = D / 8;
-        for (int i = tid; i < 32 * CH; i += 256) {
-            const int row = i / CH, c = i - row * CH;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (q0 + row < S) {
-                const long slot = (long)grp * S + q0 + row;
-                if (!P.out_rows || P.out_rows[slot] >= 0) v = *reinterpret_cast<const uint4 *>(P.q + slot * P.row_stride + (long)head * D + c * 8);
-            }
-            *reinterpret_cast<uint4 *>(Qs + row * C::VP + c * 8) = v;
-        }
-        __syncthreads();
-        for (int i = tid; i < 32 * (C::EW / 8); i += 256) {
-            const int row = i / (C::EW / 8), c = i % (C::EW / 8), tab = c * 8 >= C::WK, y0 = c * 8 - tab * C::WK;
-            if (q0 + row >= S || y0 >= w) continue;
-            const int cell = P.sigma[(long)grp * P.sigma_stride + q0 + row], r = cell / w, t0 = (tab ? cell - r * w : r) + w - 1 - y0;
-            const f16x8 g = *reinterpret_cast<const f16x8 *>(P.gsum + ((long)gh * S + q0 + row) * C::EW + c * 8);
-            const float unit = P.gunit[(long)gh * S + q0 + row];
-            bf16 *to = Gs + row * GP + tab * 2 * C::WK + t0;
+        // row j of the step is query (gh, x): the one in row R and column x (tab 1: column R, row x) of group gh / h
+        auto place = [&](int j, int &gh) {
+            const long k = k0 + j;
+            if (k >= last) return -1;
+            gh = (int)(k / w);
+            const int x = (int)(k - (long)gh * w), cell = tab ? x * w + R : R * w + x;
+            const int at = P.inverse[(P.sigma_stride ? (long)(gh / P.h) * S : 0) + cell];
+            return min(max(at, 0), S - 1);
+        };
+        for (int i = tid; i < TABLE_QUERIES * GC; i += 256) {
+            const int j = i / GC, c = i % GC;
+            int gh = 0;
+            const int at = place(j, gh);
+            uint4 h4 = make_uint4(0, 0, 0, 0), l4 = h4;
+            if (at >= 0) {
+                const long row = (long)gh * S + at;
+                const f16x8 g = *reinterpret_cast<const f16x8 *>(P.gsum + row * C::EW + tab * C::WK + c * 8);
+                const float unit = P.gunit[row];
+                float a[8], b[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (y0 + e >= w) continue;
-                const float v = (float)g[e] * unit;
-                const bf16 hi = (bf16)v;
-                to[-e] = hi;
-                to[32 * GP - e] = (bf16)(v - (float)hi);
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            bf16x8 qt[C::DT];
-#pragma unroll
-            for (int dt = 0; dt < C::DT; ++dt) qt[dt] = transposed(Qs, C::VP, t, dt, D - 4);
-#pragma unroll
-            for (int i = 0; i < MINE; ++i) {
-                if (wave * MINE + i >= TT) continue;
-                const bf16x8 hi = transposed(Gs, GP, t, wave * MINE + i, GP - 4), lo = transposed(Gs + 32 * GP, GP, t, wave * MINE + i, GP - 4);
-#pragma unroll
-                for (int dt = 0; dt < C::DT; ++dt) {
-                    acc[i][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, qt[dt], acc[i][dt], 0, 0, 0);
-                    acc[i][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, qt[dt], acc[i][dt], 0, 0, 0);
+                for (int e = 0; e < 8; ++e) {
+                    const float v = (float)g[e] * unit;
+                    a[e] = (float)(bf16)v;
+                    b[e] = v - a[e];
                 }
+                h4 = pack_bf16x8(a);
+                l4 = pack_bf16x8(b);
+            }
+            *reinterpret_cast<uint4 *>(hi + j * St::GP + c * 8) = h4;
+            *reinterpret_cast<uint4 *>(lo + j * St::GP + c * 8) = l4;
+        }
+        for (int i = tid; i < TABLE_QUERIES * CH; i += 256) {
+            const int j = i / CH, c = i - j * CH;
+            int gh = 0;
+            const int at = place(j, gh);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (at >= 0) {
+                const int grp = gh / P.h;
+                const long slot = (long)grp * S + at;
+                if (!P.out_rows || P.out_rows[slot] >= 0) v = *reinterpret_cast<const uint4 *>(P.q + slot * P.row_stride + (long)(gh - grp * P.h) * D + c * 8);
+            }
+            *reinterpret_cast<uint4 *>(Qs + j * C::VP + c * 8) = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < St::MINE; ++i) {
+            const int tile = wave + 4 * i, mt = tile / C::DT, dt = tile - mt * C::DT;
+            if (tile >= St::TILES) continue;
+#pragma unroll
+            for (int t = 0; t < TABLE_QUERIES / 16; ++t) {
+                const bf16x8 q = transposed(Qs + 16 * t * C::VP, C::VP, 0, dt, D - 4);
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(hi + 16 * t * St::GP, St::GP, 0, mt, C::WK - 4), q, acc[i], 0, 0, 0);
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed(lo + 16 * t * St::GP, St::GP, 0, mt, C::WK - 4), q, acc[i], 0, 0, 0);
             }
         }
     }
     mfma_settle();
-    // result: lane <-> feature, register <-> relative position
-    float *to = parts + (long)blockIdx.x * 4 * C::WK * D;
+    // [table][R][slice][entry][feature]; result: lane <-> feature, register <-> entry
+    float *to = parts + (long)blockIdx.x * C::WK * D;
 #pragma unroll
-    for (int i = 0; i < MINE; ++i)
+    for (int i = 0; i < St::MINE; ++i) {
+        const int tile = wave + 4 * i, mt = tile / C::DT, c = (tile - mt * C::DT) * 32 + l32;
+        if (tile >= St::TILES) continue;
 #pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int t = (wave * MINE + i) * 32 + 8 * (r >> 2) + 4 * half + (r & 3), c = dt * 32 + l32;
-                if (wave * MINE + i < TT && c < D) to[(long)t * D + c] = acc[i][dt][r];
-            }
+        for (int r = 0; r < 16; ++r) {
+            const int y = mt * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+            if (y < w && c < D) to[(long)y * D + c] = acc[i][r];
+        }
+    }
 }
 
-// [n][2][2 WK][D] sums of slices -> bf16 tables of nrel rows.  A workgroup adds up 32 columns: eight lanes with 16 bytes each, 32 slices of the n.
+// A row of a table's gradient, the sum of H_R[R + w - 1 - t] over R and the slices.  32 features a workgroup: eight lanes with 16 bytes each, 32 shares of the terms.
 __global__ void __launch_bounds__(256)
-attn_backward_table_sums_kernel(const float4 *__restrict__ parts, int n, int table, int used, bf16 *__restrict__ drel_h, bf16 *__restrict__ drel_w)
+backward_table_sums_kernel(const float4 *__restrict__ parts, int w, int WK, int slices, int D, bf16 *__restrict__ drel_h, bf16 *__restrict__ drel_w)
 {
     __shared__ float4 lds[256];
-    const int c = threadIdx.x & 7, slice = threadIdx.x >> 3;
-    const int col = (blockIdx.x * 8 + c) * 4;                // element of the table
-    const bool in = col < used;
-    const long at = ((long)blockIdx.y * table + min(col, used - 4)) / 4;
+    const int c = threadIdx.x & 7, share = threadIdx.x >> 3, t = blockIdx.y, tab = blockIdx.z;
+    const int quad = blockIdx.x * 8 + c, quads = D / 4, first = max(0, t - w + 1), n = (min(w - 1, t) - first + 1) * slices;
+    const bool in = quad < quads;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-    for (int r = slice; r < n; r += 32) {
-        const float4 t = parts[(long)r * 2 * table / 4 + at];
-        a.x += t.x; a.y += t.y; a.z += t.z; a.w += t.w;
+    for (int i = share; i < n; i += 32) {
+        const int R = first + i / slices, y = R + w - 1 - t;
+        const float4 v = parts[((((long)tab * w + R) * slices + i % slices) * WK + y) * quads + min(quad, quads - 1)];
+        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
     }
     lds[threadIdx.x] = a;
     __syncthreads();
 #pragma unroll
     for (int half = 16; half > 0; half >>= 1) {
-        if (slice < half) {
-            const float4 t = lds[threadIdx.x + half * 8];
-            a.x += t.x; a.y += t.y; a.z += t.z; a.w += t.w;
+        if (share < half) {
+            const float4 v = lds[threadIdx.x + half * 8];
+            a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
             lds[threadIdx.x] = a;
         }
         __syncthreads();
     }
-    if (slice == 0 && in) *reinterpret_cast<uint2 *>((blockIdx.y ? drel_w : drel_h) + col) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+    if (share == 0 && in) *reinterpret_cast<uint2 *>((tab ? drel_w : drel_h) + (long)t * D + quad * 4) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
 }
 
 // ---------------------------------------------------------------- launches
 inline int entry_tiles(int w) { return w <= 16 ? 1 : w <= 32 ? 2 : w <= 64 ? 4 : 8; }
-inline long table_units(int S, long n_gh) { return n_gh * ssam_div_up(S, 32); }
-inline int table_slices(long units) { return (int)(units < 256 ? units : 256); }
+// Slices of the (group, head) of a row of a table: a thousand workgroups, of a step of 64 queries each at least
+inline int table_slices(int w, long n_gh)
+{
+    const long steps = (n_gh * w + TABLE_QUERIES - 1) / TABLE_QUERIES, n = (512 + w - 1) / w;
+    return (int)(n < steps ? n : steps);
+}
 
 // Tiles of the dense prefix have all queries to walk: with few of them, a slice of the queries each, until there are two workgroups to a CU.
 constexpr int COL_SLOTS = 512;
@@ -903,7 +1059,7 @@ inline int column_splits(long heavy, int S)
     return (int)(n < 1 ? 1 : n < most ? n : most);
 }
 
-struct BwdWorkspace { size_t zeros, tab, gsum, gunit, lse, delta, parts, total; };
+struct BwdWorkspace { size_t zeros, tab, gsum, gunit, lse, delta, e, blocks, inverse, parts, total; };
 inline BwdWorkspace workspace_layout(int groups, int S, int w, int h, int d)
 {
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -915,9 +1071,14 @@ inline BwdWorkspace workspace_layout(int groups, int S, int w, int h, int d)
     o.gunit = o.gsum + up(entries);
     o.lse = o.gunit + up(rows * 4);
     o.delta = o.lse + up(rows * 4 + 128);
-    o.parts = o.delta + up(rows * 4 + 128);
+    // one order a group at most
+    const size_t orders = (size_t)groups * ((S + 31) / 32 * 32);
+    o.e = o.delta + up(rows * 4 + 128);
+    o.blocks = o.e + up((orders + 64) * 64 * entry_tiles(w));
+    o.inverse = o.blocks + up(orders / 32 * 4);
+    o.parts = o.inverse + up(orders * 4);
     // sums of slices: of the tables' gradients, and before those of dK and dV of at most COL_SLOTS tiles
-    const size_t tables = (size_t)table_slices(table_units(S, (long)groups * h)) * 64 * entry_tiles(w) * d * 4;
+    const size_t tables = (size_t)2 * w * table_slices(w, (long)groups * h) * 16 * entry_tiles(w) * d * 4;
     const long tiles = (long)groups * h * ssam_div_up(S, 128), slots = tiles * ssam_div_up(S, 256);
     const size_t columns = S <= 256 ? 0 : (size_t)(slots < COL_SLOTS ? slots : COL_SLOTS) * 128 * 2 * d * 4;
     o.total = o.parts + up(tables > columns ? tables : columns);
@@ -937,30 +1098,38 @@ int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w
 {
     const int tiles = ssam_div_up(P.S, 128), nrel = 2 * P.w - 1;
     const unsigned grid = (unsigned)((long)tiles * ssam_div_up(P.n_gh, 8) * 8);
-    const size_t lds = rows_lds_bytes<D, NT>(nrel);
-    if (int rc = allow_lds(attn_backward_rows_kernel<D, NT>, lds); rc != SSAM_OK) return rc;
-    if (int rc = allow_lds(attn_backward_columns_kernel<D, NT>, columns_lds_bytes<D, NT>()); rc != SSAM_OK) return rc;
-    hipLaunchKernelGGL((attn_backward_rows_kernel<D, NT>), dim3(grid), dim3(256), lds, st, P, tiles);
+    // orders that all groups share are the position-only ones, whose blocks of keys are patches of the grid; those of one group alone scatter them
+    const bool local = NT == 1 || P.sigma_stride == 0;
+    constexpr bool L = !(D == 80 && NT == 4);
+    const int blocks = P.SP / 32, total = blocks * (P.sigma_stride ? P.n_gh / P.h : 1);
+    auto prepare = local && L ? backward_prepare_kernel<NT, true> : backward_prepare_kernel<NT, NT == 1>;
+    hipLaunchKernelGGL(prepare, dim3(ssam_div_up(total, 4)), dim3(256), 0, st, P, blocks, total);
+    SSAM_CHECK_LAUNCH();
+    auto rows = local ? backward_rows_kernel<D, NT, L> : backward_rows_kernel<D, NT, NT == 1>;
+    const size_t lds = local ? rows_lds_bytes<D, NT, L>(nrel) : rows_lds_bytes<D, NT, NT == 1>(nrel);
+    if (int rc = allow_lds(rows, lds); rc != SSAM_OK) return rc;
+    if (int rc = allow_lds(backward_columns_kernel<D, NT>, columns_lds_bytes<D, NT>()); rc != SSAM_OK) return rc;
+    hipLaunchKernelGGL(rows, dim3(grid), dim3(256), lds, st, P, tiles);
     SSAM_CHECK_LAUNCH();
     ColWork work;
     work.gh8 = ssam_div_up(P.n_gh, 8);
     work.heavy = ssam_div_up(min(P.n_pre * P.mask_block, P.S), 128);                // (windows: mask tiles are 32, a wave looks at its own)
     work.light = tiles - work.heavy;
     work.splits = P.mask_block == 128 ? column_splits((long)work.heavy * P.n_gh, P.S) : 1;
-    hipLaunchKernelGGL((attn_backward_columns_kernel<D, NT>), dim3((unsigned)(8L * work.gh8 * (work.heavy * work.splits + work.light))), dim3(256),
+    hipLaunchKernelGGL((backward_columns_kernel<D, NT>), dim3((unsigned)(8L * work.gh8 * (work.heavy * work.splits + work.light))), dim3(256),
                        (columns_lds_bytes<D, NT>()), st, P, work, parts);
     SSAM_CHECK_LAUNCH();
     if (work.splits > 1 && work.heavy > 0) {
         const long n = (long)P.n_gh * work.heavy * 128 * (2 * D / 8);
-        hipLaunchKernelGGL(attn_backward_join_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, P, work, D, (const float4 *)parts, n);
+        hipLaunchKernelGGL(backward_join_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, P, work, D, (const float4 *)parts, n);
         SSAM_CHECK_LAUNCH();
     }
     if (drel_h) {
-        const int per = ssam_div_up(P.S, 32), slices = table_slices(table_units(P.S, P.n_gh)), used = nrel * D;
-        hipLaunchKernelGGL((attn_backward_tables_kernel<D, NT>), dim3(slices), dim3(256), (tables_lds_bytes<D, NT>()), st, P, per, table_units(P.S, P.n_gh), parts);
+        const int slices = table_slices(P.w, P.n_gh);
+        if (int rc = allow_lds(backward_tables_kernel<D, NT>, TableStage<D, NT>::BYTES); rc != SSAM_OK) return rc;
+        hipLaunchKernelGGL((backward_tables_kernel<D, NT>), dim3(2 * P.w * slices), dim3(256), (TableStage<D, NT>::BYTES), st, P, slices, parts);
         SSAM_CHECK_LAUNCH();
-        hipLaunchKernelGGL(attn_backward_table_sums_kernel, dim3(ssam_div_up(used, 32), 2), dim3(256), 0, st, (const float4 *)parts, slices,
-                           2 * BwdCfg<D, NT>::WK * D, used, drel_h, drel_w);
+        hipLaunchKernelGGL(backward_table_sums_kernel, dim3(ssam_div_up(D, 32), nrel, 2), dim3(256), 0, st, (const float4 *)parts, P.w, BwdCfg<D, NT>::WK, slices, D, drel_h, drel_w);
         SSAM_CHECK_LAUNCH();
     }
     return SSAM_OK;
@@ -1018,6 +1187,7 @@ extern "C" int ssam_sparse_attention_backward(const void *q, const void *k, cons
     P.dq = (bf16 *)dq; P.dk = (bf16 *)dk; P.dv = (bf16 *)dv;
     P.grad_stride = grad_stride;
     P.S = S; P.w = w; P.h = h; P.n_gh = groups * h;
+    P.per_w = (uint32_t)((1 << 22) / w + 1);
     P.mask_block = mask_block;
     P.n_pre = ssam_prefix_tiles(ssam_div_up(S, mask_block), r);
     P.scale = scale;
@@ -1031,6 +1201,9 @@ extern "C" int ssam_sparse_attention_backward(const void *q, const void *k, cons
     P.delta = (float *)(ws + at.delta);
     P.zeros = (const uint4 *)(ws + at.zeros);
     P.SP = (S + 31) / 32 * 32;
+    P.e = (uint4 *)(ws + at.e);
+    P.blocks = (uint32_t *)(ws + at.blocks);
+    P.inverse = (int32_t *)(ws + at.inverse);
     float *parts = (float *)(ws + at.parts);
     hipStream_t st = (hipStream_t)stream;
     switch (d) {
