@@ -96,9 +96,9 @@ __device__ __forceinline__ f32x16 zero16()
 
 // Operand a of step t over 16 rows of an LDS block: lane <-> column 32 * tile + (lane & 31) of rows 16 t + 8 (e / 4) + 4 half + (e & 3), the order in
 // which a 32x32 result holds them.  Columns past `last` re-read that quad; what they give is not used.
-__device__ __forceinline__ bf16x8 transposed(const bf16 *block, int pitch, int t, int tile, int last)
+__device__ __forceinline__ bf16x8 transposed(const bf16 *block, int pitch, int t, int tile, int last, int lane = threadIdx.x & 63)
 {
-    const int lane = threadIdx.x & 63, li = lane & 15;
+    const int li = lane & 15;
     int col = tile * 32 + 16 * ((lane >> 4) & 1) + 4 * (li & 3);
     if (tile * 32 + 28 > last) col = min(col, last);         // (known at compile time: the others' addresses differ by constants)
     const bf16 *p = block + (16 * t + 4 * (lane >> 5) + (li >> 2)) * pitch + col;
@@ -113,6 +113,19 @@ __device__ __forceinline__ bf16x8 half_of(const f32x16 &s, int t)
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = (bf16)s[8 * t + e];
     return p;
+}
+
+// The lane, not known from before: what follows from it is worked out where it is used instead of kept in registers through a walk.
+__device__ __forceinline__ int lane_now()
+{
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+// the other half-wave's value
+__device__ __forceinline__ float other_half(float x)
+{
+    return __int_as_float(__builtin_amdgcn_ds_bpermute((lane_now() ^ 32) * 4, __float_as_int(x)));
 }
 
 // 32 rows held as [column tiles]^T results -> bf16 rows in memory, through the wave's LDS: whole rows of 16-byte stores.  row < 0: not stored.
@@ -167,10 +180,11 @@ template <int CHUNKS>
 struct Transposed {
     static constexpr int PITCH = CHUNKS * 16;
     static constexpr int KINDS = CHUNKS == 8 ? 2 : 1;         // (rows of 16 chunks and more: the place of another tile is the first one's with bits changed)
-    int at[KINDS][2];
-    __device__ __forceinline__ Transposed()
+    int at[KINDS][2], again;
+    __device__ __forceinline__ Transposed(int lane = threadIdx.x & 63)
     {
-        const int lane = threadIdx.x & 63, li = lane & 15;
+        again = ((lane >> 4) & 1) * 32;
+        const int li = lane & 15;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int r = 8 * u + 4 * (lane >> 5) + (li >> 2), f0 = (CHUNKS == 2 ? 0 : 16 * ((lane >> 4) & 1)) + 4 * (li & 3);
@@ -186,7 +200,7 @@ struct Transposed {
         for (int u = 0; u < 2; ++u) {
             int a = CHUNKS >= 16 ? (at[0][u] ^ (tile & 3) * 64) + base + 16 * t * PITCH + tile / 4 * 256
                                  : at[tile % KINDS][u] + base + 16 * t * PITCH + tile / KINDS * KINDS * 64;
-            if (CHUNKS == 10 && tile == 2) a -= ((threadIdx.x >> 4) & 1) * 32;
+            if (CHUNKS == 10 && tile == 2) a -= again;
             v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(smem + a));
         }
         return bf16x8{ v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3] };
@@ -198,9 +212,9 @@ template <int CHUNKS>
 struct Straight {
     static constexpr bool LINE = CHUNKS == 2 || CHUNKS == 10;   // the swizzle changes places by twos: those of a step are 32 bytes from the last one's
     int at[LINE ? 1 : CHUNKS / 2];
-    __device__ __forceinline__ Straight()
+    __device__ __forceinline__ Straight(int lane = threadIdx.x & 63)
     {
-        const int lane = threadIdx.x & 63, l32 = lane & 31;
+        const int l32 = lane & 31;
 #pragma unroll
         for (int ks = 0; ks < (LINE ? 1 : CHUNKS / 2); ++ks) at[ks] = l32 * CHUNKS * 16 + ((2 * ks + (lane >> 5)) ^ swizzle<CHUNKS>(l32)) * 16;
     }
@@ -1013,19 +1027,20 @@ backward_tables_kernel(BwdParams P, int slices, float *__restrict__ parts)
     }
 }
 
-// A row of a table's gradient, the sum of H_R[R + w - 1 - t] over R and the slices.  32 features a workgroup: eight lanes with 16 bytes each, 32 shares of the terms.
+// A row of a table's gradient: the sum of H_R[R + w - 1 - t] over R and the slices, or (WINDOWS) of the row itself over the workgroups that have summed it.  32 features a workgroup: eight lanes with 16 bytes each, 32 shares of the terms.
+template <bool WINDOWS>
 __global__ void __launch_bounds__(256)
 backward_table_sums_kernel(const float4 *__restrict__ parts, int w, int WK, int slices, int D, bf16 *__restrict__ drel_h, bf16 *__restrict__ drel_w)
 {
     __shared__ float4 lds[256];
     const int c = threadIdx.x & 7, share = threadIdx.x >> 3, t = blockIdx.y, tab = blockIdx.z;
-    const int quad = blockIdx.x * 8 + c, quads = D / 4, first = max(0, t - w + 1), n = (min(w - 1, t) - first + 1) * slices;
+    const int quad = blockIdx.x * 8 + c, quads = D / 4, first = max(0, t - w + 1), n = WINDOWS ? slices : (min(w - 1, t) - first + 1) * slices;
     const bool in = quad < quads;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
     for (int i = share; i < n; i += 32) {
         const int R = first + i / slices, y = R + w - 1 - t;
-        const float4 v = parts[((((long)tab * w + R) * slices + i % slices) * WK + y) * quads + min(quad, quads - 1)];
+        const float4 v = parts[(WINDOWS ? ((long)i * 2 + tab) * 32 + t : (((long)tab * w + R) * slices + i % slices) * WK + y) * quads + min(quad, quads - 1)];
         a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
     }
     lds[threadIdx.x] = a;
@@ -1041,6 +1056,12 @@ backward_table_sums_kernel(const float4 *__restrict__ parts, int w, int WK, int 
     }
     if (share == 0 && in) *reinterpret_cast<uint2 *>((tab ? drel_w : drel_h) + (long)t * D + quad * 4) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
 }
+
+}  // namespace
+
+#include "attention_backward_window.h"
+
+namespace {
 
 // ---------------------------------------------------------------- launches
 inline int entry_tiles(int w) { return w <= 16 ? 1 : w <= 32 ? 2 : w <= 64 ? 4 : 8; }
@@ -1058,6 +1079,8 @@ inline int column_splits(long heavy, int S)
     const long most = (S + 255) / 256, n = COL_SLOTS / (heavy > 0 ? heavy : 1);
     return (int)(n < 1 ? 1 : n < most ? n : most);
 }
+
+inline int window_groups(long n_gh) { return (int)(n_gh < WIN_GROUPS ? n_gh : WIN_GROUPS); }
 
 struct BwdWorkspace { size_t zeros, tab, gsum, gunit, lse, delta, e, blocks, inverse, parts, total; };
 inline BwdWorkspace workspace_layout(int groups, int S, int w, int h, int d)
@@ -1081,7 +1104,8 @@ inline BwdWorkspace workspace_layout(int groups, int S, int w, int h, int d)
     const size_t tables = (size_t)2 * w * table_slices(w, (long)groups * h) * 16 * entry_tiles(w) * d * 4;
     const long tiles = (long)groups * h * ssam_div_up(S, 128), slots = tiles * ssam_div_up(S, 256);
     const size_t columns = S <= 256 ? 0 : (size_t)(slots < COL_SLOTS ? slots : COL_SLOTS) * 128 * 2 * d * 4;
-    o.total = o.parts + up(tables > columns ? tables : columns);
+    const size_t windows = S > WIN_ROWS ? 0 : (size_t)window_groups((long)groups * h) * 2 * 32 * d * 4, most = tables > columns ? tables : columns;
+    o.total = o.parts + up(most > windows ? most : windows);
     return o;
 }
 
@@ -1098,8 +1122,9 @@ int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w
 {
     const int tiles = ssam_div_up(P.S, 128), nrel = 2 * P.w - 1;
     const unsigned grid = (unsigned)((long)tiles * ssam_div_up(P.n_gh, 8) * 8);
-    // orders that all groups share are the position-only ones, whose blocks of keys are patches of the grid; those of one group alone scatter them
-    const bool local = NT == 1 || P.sigma_stride == 0;
+    // orders that all groups share are the position-only ones, whose blocks of keys are patches of a grid of a power of two (28 x 28, where they are not: 67 us against 45);
+    // those of one group alone scatter them
+    const bool local = NT == 1 || (P.sigma_stride == 0 && (P.w & (P.w - 1)) == 0);
     constexpr bool L = !(D == 80 && NT == 4);
     const int blocks = P.SP / 32, total = blocks * (P.sigma_stride ? P.n_gh / P.h : 1);
     auto prepare = local && L ? backward_prepare_kernel<NT, true> : backward_prepare_kernel<NT, NT == 1>;
@@ -1129,7 +1154,21 @@ int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w
         if (int rc = allow_lds(backward_tables_kernel<D, NT>, TableStage<D, NT>::BYTES); rc != SSAM_OK) return rc;
         hipLaunchKernelGGL((backward_tables_kernel<D, NT>), dim3(2 * P.w * slices), dim3(256), (TableStage<D, NT>::BYTES), st, P, slices, parts);
         SSAM_CHECK_LAUNCH();
-        hipLaunchKernelGGL(backward_table_sums_kernel, dim3(ssam_div_up(D, 32), nrel, 2), dim3(256), 0, st, (const float4 *)parts, P.w, BwdCfg<D, NT>::WK, slices, D, drel_h, drel_w);
+        hipLaunchKernelGGL((backward_table_sums_kernel<false>), dim3(ssam_div_up(D, 32), nrel, 2), dim3(256), 0, st, (const float4 *)parts, P.w, BwdCfg<D, NT>::WK, slices, D, drel_h, drel_w);
+        SSAM_CHECK_LAUNCH();
+    }
+    return SSAM_OK;
+}
+
+template <int D>
+int launch_windows(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w, hipStream_t st)
+{
+    const int groups = window_groups(P.n_gh), nrel = 2 * P.w - 1;
+    if (int rc = allow_lds(backward_windows_kernel<D>, WinCfg<D>::TOTAL); rc != SSAM_OK) return rc;
+    hipLaunchKernelGGL((backward_windows_kernel<D>), dim3(groups), dim3(64 * WIN_WAVES), WinCfg<D>::TOTAL, st, P, drel_h != nullptr, parts);
+    SSAM_CHECK_LAUNCH();
+    if (drel_h) {
+        hipLaunchKernelGGL((backward_table_sums_kernel<true>), dim3(ssam_div_up(D, 32), nrel, 2), dim3(256), 0, st, (const float4 *)parts, P.w, 32, groups, D, drel_h, drel_w);
         SSAM_CHECK_LAUNCH();
     }
     return SSAM_OK;
@@ -1138,6 +1177,7 @@ int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w
 template <int D>
 int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w, hipStream_t st)
 {
+    if (P.S <= WIN_ROWS) return launch_windows<D>(P, parts, drel_h, drel_w, st);
     switch (entry_tiles(P.w)) {
     case 1: return launch_backward<D, 1>(P, parts, drel_h, drel_w, st);
     case 2: return launch_backward<D, 2>(P, parts, drel_h, drel_w, st);
