@@ -192,6 +192,13 @@ struct Transposed {
             for (int k = 0; k < KINDS; ++k) at[k][u] = r * PITCH + ((4 * k + (f0 >> 3)) ^ swizzle<CHUNKS>(r)) * 16 + (f0 & 7) * 2;
         }
     }
+    // place of quad u of a tile that is known only when the kernel runs
+    __device__ __forceinline__ int place(int u, int tile) const
+    {
+        if (CHUNKS == 10) return at[0][u] + tile * 64 - (tile == 2 ? again : 0);
+        if (CHUNKS == 8) return at[0][u] ^ ((at[0][u] ^ at[KINDS - 1][u]) & -(tile & 1));
+        return at[0][u];
+    }
     // base: byte offset of the block in LDS.  (Of a last tile that the rows fill by half, 10 chunks, the other half is the same columns again.)
     __device__ __forceinline__ bf16x8 operator()(const unsigned char *smem, int base, int t, int tile) const
     {

@@ -17,8 +17,7 @@ template <int D>
 struct WinCfg {
     using C = BwdCfg<D, 1>;
     static constexpr int RB = D * 2, EB = C::EW * 2, GB = 128;                      // rows, in bytes; of G: 2 x 32 relative positions
-    static constexpr int Q = 0, O = Q + WIN_ROWS * RB, UEND = WIN_TILES * 32 * C::UP * 2, OEND = O + WIN_ROWS * RB;
-    static constexpr int K = OEND > UEND ? OEND : UEND, V = K + WIN_ROWS * RB;      // (up to UEND lie products with the tables before Q and dO do)
+    static constexpr int Q = 0, O = Q + WIN_ROWS * RB, K = O + WIN_ROWS * RB, V = K + WIN_ROWS * RB;
     static constexpr int G = K, GPART = WIN_ROWS * GB, REL = G + 2 * GPART, REND = REL + 2 * 32 * C::VP * 2;
     static constexpr int VEND = V + WIN_ROWS * RB, E = VEND > REND ? VEND : REND;
     static constexpr int L = E + WIN_ROWS * EB, N = L + WIN_ROWS * 4, TOTAL = N + WIN_ROWS * 4;
@@ -26,19 +25,21 @@ struct WinCfg {
     static_assert(TOTAL <= 160 * 1024 && (WIN_TILES - 1) * PART <= TOTAL, "");
 };
 
-// 32 result rows [column tiles]^T straight to memory, eight bytes a lane: two half-waves fill 16 bytes of a row, and the cache puts rows together
+// 32 result rows [column tiles]^T straight to memory: of two groups of eight features a half-wave takes one each, 16 bytes a lane
 template <int D>
 __device__ __forceinline__ void store_direct(const f32x16 *acc, bf16 *row, bool stored)
 {
     const int half = lane_now() >> 5;
-    if (!stored) return;
 #pragma unroll
-    for (int dt = 0; dt < (D + 31) / 32; ++dt)
+    for (int c = 0; c < D / 8; c += 2) {
+        uint32_t x[2][2];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            if (dt * 32 + 8 * g >= D) continue;
-            *reinterpret_cast<bf16x4 *>(row + dt * 32 + 8 * g + 4 * half) = bf16x4{ (bf16)acc[dt][4 * g], (bf16)acc[dt][4 * g + 1], (bf16)acc[dt][4 * g + 2], (bf16)acc[dt][4 * g + 3] };
-        }
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[g][i] = pack_bf16x2(acc[(c + g) / 4][(c + g) % 4 * 4 + 2 * i], acc[(c + g) / 4][(c + g) % 4 * 4 + 2 * i + 1]);
+        const auto a = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false), b = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+        if (stored) *reinterpret_cast<uint4 *>(row + (c + half) * 8) = make_uint4(a[0], b[0], a[1], b[1]);
+    }
 }
 
 template <int D>
@@ -70,90 +71,107 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
         const int esw = swizzle<EC>(l32) ^ half, fsw = swizzle<CH>(l32) ^ half;
         const bf16 *rel_h = P.rel_h, *rel_w = P.rel_w;
         asm volatile("" : "+s"(rel_h), "+s"(rel_w));           // (read again for every (group, head): kept, their rows would take 40 registers)
-        const long slot = (long)grp * S + min(pos, S - 1);
         const int rc = row_col(P.sigma + (long)grp * P.sigma_stride, pos, P), row = rc & 0xffff, col = rc >> 16;
-        bf16x8 qf[C::KS], of[C::KS];
-        float delta = 0.f;
-        f16x8 bt[2];
-        const int orow = pos < S ? P.out_rows ? P.out_rows[slot] : 0 : -1;
+        // Features of all rows, 16 bytes a thread and whole rows by neighbouring threads (a wave that reads its own operands' places asks for twice as many lines, and the requests are
+        // what bounds this); parts of dO . O go where E comes to lie.  Rows past the end, and of queries whose output is dropped, are zeros.
+        constexpr int LOADS = (WIN_ROWS * CH + 64 * WIN_WAVES - 1) / (64 * WIN_WAVES);
+        bf16x8 rf[2][C::KS];
         {
-            bf16x8 kf[C::KS], vf[C::KS];
+            u32x4 x[5][LOADS];
+            uint32_t live = 0;                                // bit k: the row exists, bit 16 + k: and its output is not dropped
+            int outs[LOADS];
+            if (P.out_rows) {
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks)
+                for (int k = 0; k < LOADS; ++k) outs[k] = P.out_rows[(long)grp * S + min((tid + 64 * WIN_WAVES * k) / CH, S - 1)];
+            } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) qf[ks][e] = of[ks][e] = kf[ks][e] = vf[ks][e] = (bf16)0.f;
-            if (pos < S) {
-                const long from = slot * P.row_stride + (long)head * D + half * 8;
-#pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) {
-                    kf[ks] = *reinterpret_cast<const bf16x8 *>(P.k + from + ks * 16);
-                    vf[ks] = *reinterpret_cast<const bf16x8 *>(P.v + from + ks * 16);
-                }
-                if (orow >= 0) {                              // (else its output is dropped: no gradient comes from it)
-                    const long at = (P.out_rows ? (long)orow : slot) * ((long)P.h * D) + (long)head * D + half * 8;
-#pragma unroll
-                    for (int ks = 0; ks < C::KS; ++ks) {
-                        qf[ks] = *reinterpret_cast<const bf16x8 *>(P.q + from + ks * 16);
-                        of[ks] = *reinterpret_cast<const bf16x8 *>(P.dout + at + ks * 16);
-                        const bf16x8 o = *reinterpret_cast<const bf16x8 *>(P.out + at + ks * 16);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) delta = fmaf((float)of[ks][e], (float)o[e], delta);
-                    }
-                }
+                for (int k = 0; k < LOADS; ++k) outs[k] = 0;
             }
+            // (no branch around a load: all of them are asked for before the first is waited for)
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) {
+                const int i = tid + 64 * WIN_WAVES * k, r = i / CH, c = i - r * CH;
+                const long at = (long)grp * S + min(r, S - 1), from = at * P.row_stride + (long)head * D + c * 8;
+                const long place = (P.out_rows ? (long)max(outs[k], 0) : at) * ((long)P.h * D) + (long)head * D + c * 8;
+                live |= r < S ? outs[k] >= 0 ? 0x10001u << k : 1u << k : 0u;
+                x[0][k] = *reinterpret_cast<const u32x4 *>(P.k + from);
+                x[1][k] = *reinterpret_cast<const u32x4 *>(P.v + from);
+                x[2][k] = *reinterpret_cast<const u32x4 *>(P.q + from);
+                x[3][k] = *reinterpret_cast<const u32x4 *>(P.dout + place);
+                x[4][k] = *reinterpret_cast<const u32x4 *>(P.out + place);
+            }
+#pragma unroll
+            for (int tab = 0; tab < 2; ++tab)
+#pragma unroll
+                for (int ks = 0; ks < C::KS; ++ks) rf[tab][ks] = *reinterpret_cast<const bf16x8 *>((tab ? rel_w : rel_h) + (long)min(l32, nrel - 1) * D + half * 8 + ks * 16);
             __syncthreads();                                 // nobody reads the (group, head) before any more
-            if (alive) {
 #pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) {
-                    unsigned char *to = smem + pos * W::RB + ((2 * ks) ^ fsw) * 16;
-                    *reinterpret_cast<bf16x8 *>(to + W::K) = kf[ks];
-                    *reinterpret_cast<bf16x8 *>(to + W::V) = vf[ks];
-                }
-                // E: a half-wave has the row's 16 entries, the other one the column's
+            for (int k = 0; k < LOADS; ++k) {
+                const int i = tid + 64 * WIN_WAVES * k, r = i / CH, c = i - r * CH;
+                if (r >= WIN_ROWS) continue;
+                unsigned char *to = smem + r * W::RB + (c ^ swizzle<CH>(r)) * 16;
+                const bf16x8 d = __builtin_bit_cast(bf16x8, x[3][k]), o = __builtin_bit_cast(bf16x8, x[4][k]);
+                float dot = 0.f;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    *reinterpret_cast<f16x8 *>(smem + W::E + pos * W::EB + ((2 * half + c) ^ swizzle<EC>(l32)) * 16) = ones((half ? col : row) - 8 * c);
+                for (int e = 0; e < 8; ++e) dot = fmaf((float)d[e], (float)o[e], dot);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) x[n][k] = live >> (n < 2 ? k : 16 + k) & 1 ? x[n][k] : u32x4{ 0, 0, 0, 0 };
+                *reinterpret_cast<u32x4 *>(to + W::K) = x[0][k];
+                *reinterpret_cast<u32x4 *>(to + W::V) = x[1][k];
+                *reinterpret_cast<u32x4 *>(to + W::Q) = x[2][k];
+                *reinterpret_cast<u32x4 *>(to + W::O) = x[3][k];
+                *reinterpret_cast<float *>(smem + W::E + r * W::EB + c * 4) = live >> (16 + k) & 1 ? dot : 0.f;
             }
         }
-        delta += other_half(delta);
+        const Straight<CH> fa(lane);
+        bf16x8 qf[C::KS], of[C::KS];
+        f16x8 bt[2] = { { 0, 0, 0, 0, 0, 0, 0, 0 }, { 0, 0, 0, 0, 0, 0, 0, 0 } };
+        float delta = 0.f;
+        __syncthreads();
+        // (a wave behind the last tile reads what lies behind, so that these are not undefined on any way: the compiler would keep the last ones)
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks) {
+            qf[ks] = fa(smem, W::Q + 32 * wave * W::RB, ks);
+            of[ks] = fa(smem, W::O + 32 * wave * W::RB, ks);
+        }
         if (alive) {
-            // bias entries over the scale: rel Q^T, whose 32 rows hold all relative positions (w <= 14), and the entries back from where they lie for this query
-            constexpr int FIRST = 2 * C::WK;
-            _Float16 *u_row = reinterpret_cast<_Float16 *>(smem) + (wave * 32 + l32) * C::UP;
+            unsigned char *mine = smem + W::E + pos * W::EB;
+#pragma unroll
+            for (int c = 0; c < CH; c += 2) delta += *reinterpret_cast<const float *>(mine + (c + half) * 4);
+            delta += other_half(delta);
+            const int usw = l32 >> 2 & 7;                     // (rows of 64 bytes: four eight-byte places apart share banks without it)
+            // bias entries over the scale: rel Q^T, whose 32 rows hold all relative positions (w <= 14) and fill the query's row of E for now; entry y is position t0 - y
 #pragma unroll
             for (int tab = 0; tab < 2; ++tab) {
-                wave_lds_fence();
-                _Float16 *to = u_row + (FIRST + w - 1 + (tab ? col : row) - 4 * half);
-                const bf16 *rp = (tab ? rel_w : rel_h) + (long)min(l32, nrel - 1) * D + half * 8;
                 f32x16 u = zero16();
 #pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(rp + ks * 16), qf[ks], u, 0, 0, 0);
+                for (int ks = 0; ks < C::KS; ++ks) u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rf[tab][ks], qf[ks], u, 0, 0, 0);
                 mfma_settle();
-#pragma unroll
-                for (int r = 0; r < 16; ++r) to[-8 * (r >> 2) - (r & 3)] = (_Float16)(u[r] * P.inv_scale);
                 wave_lds_fence();
-                f16x8 v = *reinterpret_cast<const f16x8 *>(u_row + FIRST + 8 * half);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 8 * half + e < w ? v[e] : (_Float16)0.f;
-                bt[tab] = v;
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f16x4 *>(mine + ((2 * g + half) ^ usw) * 8) = f16x4{ (_Float16)(u[4 * g] * P.inv_scale), (_Float16)(u[4 * g + 1] * P.inv_scale), (_Float16)(u[4 * g + 2] * P.inv_scale),
+                                                                                      (_Float16)(u[4 * g + 3] * P.inv_scale) };
+                wave_lds_fence();
+                const int t0 = (tab ? col : row) + w - 1 - 8 * half;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = max(t0 - e, 0);
+                    const _Float16 x = *reinterpret_cast<const _Float16 *>(mine + ((t >> 2) ^ usw) * 8 + (t & 3) * 2);
+                    bt[tab][e] = 8 * half + e < w ? x : (_Float16)0.f;
+                }
             }
+            wave_lds_fence();
+            // E: a half-wave has the row's 16 entries, the other one the column's
+#pragma unroll
+            for (int c = 0; c < 2; ++c) *reinterpret_cast<f16x8 *>(mine + ((2 * half + c) ^ swizzle<EC>(l32)) * 16) = ones((half ? col : row) - 8 * c);
         }
         __syncthreads();
-        if (alive)
-#pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) {
-                unsigned char *to = smem + pos * W::RB + ((2 * ks) ^ fsw) * 16;
-                *reinterpret_cast<bf16x8 *>(to + W::Q) = qf[ks];
-                *reinterpret_cast<bf16x8 *>(to + W::O) = of[ks];
-            }
-        // (Q and dO are read behind the rows' barrier; K, V and E were written in front of the one above)
-
         const Transposed<CH> ft(lane);
-        const Straight<CH> fa(lane);
 
         // ---- rows
         const Transposed<EC> et(lane);
-        // (of 80 features dO comes back from LDS for every block, and V is not read along with K: registers for them are short)
+        // (of 80 features Q and dO come back from LDS for every block: registers for them are short)
         f32x16 acc[C::DT], gt = zero16();
 #pragma unroll
         for (int t = 0; t < C::DT; ++t) acc[t] = zero16();
@@ -164,11 +182,11 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
             const int at = 32 * j * W::RB;
             const unsigned char *el = smem + W::E + (32 * j + l32) * W::EB;
             f32x16 sc = zero16(), dp = zero16();
+            if (D == 80) asm volatile("" : "+v"(bt[0]), "+v"(bt[1]));       // (else the compiler puts them into scratch memory)
             sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(el + esw * 16), bt[0], sc, 0, 0, 0);
             sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const f16x8 *>(el + (2 ^ esw) * 16), bt[1], sc, 0, 0, 0);
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa(smem, at + W::K, ks), qf[ks], sc, 0, 0, 0);
-            if (D == 80) asm volatile("" : "+v"(bt[0]), "+v"(bt[1]));
+            for (int ks = 0; ks < C::KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa(smem, at + W::K, ks), D == 80 ? fa(smem, W::Q + 32 * wave * W::RB, ks) : qf[ks], sc, 0, 0, 0);
 #pragma unroll
             for (int ks = 0; ks < C::KS; ++ks) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa(smem, at + W::V, ks), D == 80 ? fa(smem, W::O + 32 * wave * W::RB, ks) : of[ks], dp, 0, 0, 0);
             const int left = S - 32 * j - 4 * half;           // keys past the end
@@ -207,12 +225,29 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
             }
         }
         mfma_settle();
+        constexpr int RELS = (64 * CH + 64 * WIN_WAVES - 1) / (64 * WIN_WAVES);
+        u32x4 rv[RELS];                                      // 32 rows a table, zeros behind its own
+#pragma unroll
+        for (int k = 0; k < RELS; ++k) {
+            const int i = tid + 64 * WIN_WAVES * k, r = i / CH, c = i - r * CH;
+            rv[k] = u32x4{ 0, 0, 0, 0 };
+            if (r < 64 && (r & 31) < nrel) rv[k] = *reinterpret_cast<const u32x4 *>((r < 32 ? rel_h : rel_w) + (long)(r & 31) * D + c * 8);
+        }
+        // a wave's first keys on columns
+        const int tile0 = light < tiles ? light : dense < heavy ? dense : 0;
+        bf16x8 kf[C::KS], vf[C::KS];
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks) {
+            kf[ks] = fa(smem, W::K + 32 * tile0 * W::RB, ks);
+            vf[ks] = fa(smem, W::V + 32 * tile0 * W::RB, ks);
+        }
         __syncthreads();                                     // K, V and E are read
         if (alive) {
             l += other_half(l);
             const float inv = 1.f / l;
             if (half == 0) {
-                reinterpret_cast<float *>(smem + W::L)[pos] = orow < 0 ? -INFINITY : -(m + __builtin_amdgcn_logf(l)) * P.inv_scale_log2e;
+                const bool none = pos >= S || (P.out_rows && P.out_rows[(long)grp * S + pos] < 0);
+                reinterpret_cast<float *>(smem + W::L)[pos] = none ? -INFINITY : -(m + __builtin_amdgcn_logf(l)) * P.inv_scale_log2e;
                 reinterpret_cast<float *>(smem + W::N)[pos] = -delta;
             }
 #pragma unroll
@@ -226,27 +261,25 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
             const int gsw = swizzle<8>(l32);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                *reinterpret_cast<uint4 *>(mine + (4 * half + c) * 16) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(mine + W::GPART + (4 * half + c) * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(mine + ((4 * half + c) ^ gsw) * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(mine + W::GPART + ((4 * half + c) ^ gsw) * 16) = make_uint4(0, 0, 0, 0);
             }
             wave_lds_fence();
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int y = 8 * (r >> 2 & 1) + 4 * half + (r & 3), at = 32 * (r >> 3) + (r >> 3 ? col : row) + w - 1 - y;
+                // (entries from w on are zeros: they go to positions that are none, below the first one's or, from the front of the row, to its end)
+                const int y = 8 * (r >> 2 & 1) + 4 * half + (r & 3), at = 32 * (r >> 3) + (((r >> 3 ? col : row) + w - 1 - y) & 31);
                 const float x = gt[r] * (inv * 128.f);
                 const bf16 hi = (bf16)x;
-                if (y < w) {
-                    bf16 *to = reinterpret_cast<bf16 *>(mine + ((at >> 3) ^ gsw) * 16) + (at & 7);
-                    *to = hi;
-                    to[W::GPART / 2] = (bf16)(x - (float)hi);
-                }
+                bf16 *to = reinterpret_cast<bf16 *>(mine + ((at >> 3) ^ gsw) * 16) + (at & 7);
+                *to = hi;
+                to[W::GPART / 2] = (bf16)(x - (float)hi);
             }
         }
-        for (int i = tid; i < 64 * CH; i += 64 * WIN_WAVES) {
-            const int r = i / CH, c = i - r * CH;
-            u32x4 v = { 0, 0, 0, 0 };
-            if ((r & 31) < nrel) v = *reinterpret_cast<const u32x4 *>((r < 32 ? rel_h : rel_w) + (long)(r & 31) * D + c * 8);
-            *reinterpret_cast<u32x4 *>(smem + W::REL + (r * C::VP + c * 8) * 2) = v;
+#pragma unroll
+        for (int k = 0; k < RELS; ++k) {
+            const int i = tid + 64 * WIN_WAVES * k, r = i / CH, c = i - r * CH;
+            if (i < 64 * CH) *reinterpret_cast<u32x4 *>(smem + W::REL + (r * C::VP + c * 8) * 2) = rv[k];
         }
         __syncthreads();
         if (alive) {
@@ -278,22 +311,25 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
         if (tables && wave < 2 * C::DT) {
             const int tab = wave / C::DT, dt = wave % C::DT;
             const Transposed<8> gtr(lane);
+            int f0 = W::Q + ft.place(0, dt), f1 = W::Q + ft.place(1, dt), g0 = W::G + gtr.place(0, tab), g1 = W::G + gtr.place(1, tab);
+            const auto read = [&](int at0, int at1) __attribute__((always_inline)) {
+                const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(smem + at0));
+                const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4 *)(smem + at1));
+                return bf16x8{ a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3] };
+            };
 #pragma unroll 1
-            for (int i = 0; i < tiles; ++i)
+            for (int i = 0; i < tiles; ++i) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    // (the place of a tile is part of a constant where the rows' pitch asks for it: one of three features' tiles, one of two tables)
-                    bf16x8 f;
-                    if (dt == 0) f = ft(smem, W::Q + 32 * i * W::RB, t, 0);
-                    else if (dt == 1) f = ft(smem, W::Q + 32 * i * W::RB, t, 1 % C::DT);
-                    else f = ft(smem, W::Q + 32 * i * W::RB, t, 2 % C::DT);
-#pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        const int at = W::G + part * W::GPART + 32 * i * W::GB;
-                        const bf16x8 g = tab ? gtr(smem, at, t, 1) : gtr(smem, at, t, 0);
-                        table = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g, f, table, 0, 0, 0);
-                    }
+                    const bf16x8 f = read(f0 + 16 * t * W::RB, f1 + 16 * t * W::RB);
+                    table = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read(g0 + 16 * t * W::GB, g1 + 16 * t * W::GB), f, table, 0, 0, 0);
+                    table = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read(g0 + 16 * t * W::GB + W::GPART, g1 + 16 * t * W::GB + W::GPART), f, table, 0, 0, 0);
                 }
+                f0 += 32 * W::RB;
+                f1 += 32 * W::RB;
+                g0 += 32 * W::GB;
+                g1 += 32 * W::GB;
+            }
         }
 
         // ---- columns
@@ -305,12 +341,13 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
             const int tile = pass ? dense : light, i0 = pass ? share * per : tile >> mb << mb, i1 = min(i0 + (pass ? per : 1 << mb), tiles);
             if (tile >= (pass ? heavy : tiles)) continue;     // the same for the whole wave
             const int kpos = tile * 32 + l32;
-            const long kslot = (long)grp * S + min(kpos, S - 1);      // keys past the end repeat the last one; their results are not stored
-            bf16x8 kf[C::KS], vf[C::KS];
+            if (tile != tile0) {                             // (keys past the end repeat the last one; their results are not stored)
+                const long from = ((long)grp * S + min(kpos, S - 1)) * P.row_stride + (long)head * D + half * 8;
 #pragma unroll
-            for (int ks = 0; ks < C::KS; ++ks) {
-                kf[ks] = *reinterpret_cast<const bf16x8 *>(P.k + kslot * P.row_stride + (long)head * D + half * 8 + ks * 16);
-                vf[ks] = *reinterpret_cast<const bf16x8 *>(P.v + kslot * P.row_stride + (long)head * D + half * 8 + ks * 16);
+                for (int ks = 0; ks < C::KS; ++ks) {
+                    kf[ks] = *reinterpret_cast<const bf16x8 *>(P.k + from + ks * 16);
+                    vf[ks] = *reinterpret_cast<const bf16x8 *>(P.v + from + ks * 16);
+                }
             }
             const int krc = row_col(P.sigma + (long)grp * P.sigma_stride, kpos, P);
             const f16x8 er = ones((krc & 0xffff) - 8 * half), ec = ones((krc >> 16) - 8 * half);
