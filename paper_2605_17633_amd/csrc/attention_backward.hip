@@ -1172,7 +1172,8 @@ int launch_windows(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w,
 {
     const int groups = window_groups(P.n_gh), nrel = 2 * P.w - 1;
     if (int rc = allow_lds(backward_windows_kernel<D>, WinCfg<D>::TOTAL); rc != SSAM_OK) return rc;
-    hipLaunchKernelGGL((backward_windows_kernel<D>), dim3(groups), dim3(64 * WIN_WAVES), WinCfg<D>::TOTAL, st, P, drel_h != nullptr, parts);
+    hipLaunchKernelGGL((backward_windows_kernel<D>), dim3(groups), dim3(64 * WIN_WAVES), WinCfg<D>::TOTAL, st, P,
+                       window_work(ssam_div_up(P.S, 32), min(P.n_pre * (P.mask_block / 32), ssam_div_up(P.S, 32)), P.mask_block / 32), drel_h != nullptr, parts);
     SSAM_CHECK_LAUNCH();
     if (drel_h) {
         hipLaunchKernelGGL((backward_table_sums_kernel<true>), dim3(ssam_div_up(D, 32), nrel, 2), dim3(256), 0, st, (const float4 *)parts, P.w, 32, groups, D, drel_h, drel_w);

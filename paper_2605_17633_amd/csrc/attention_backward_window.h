@@ -5,13 +5,32 @@
 //   rows     wave i has the queries of tile i (32): scores, P, dS over its keys; leaves dQ, G, -log sum exp
 //   tables   a 32 x 32 tile of drel a wave, over all queries
 //   columns  every active (query tile, key tile) once more with P from the statistics.  Keys of the dense prefix see all queries: their query tiles are dealt out to several waves,
-//            whose sums are added through LDS in order; the others see one tile of the mask, and a wave has at most one of them, in front of its share of the prefix
+//            whose sums are added through LDS in order; the others see one tile of the mask
 // The space of K and V holds G (as the sum of two bf16) and the relative positions' features once the rows are done; that of E then holds the bias entries T.
 #pragma once
 
 namespace {
 
 constexpr int WIN_ROWS = 224, WIN_TILES = WIN_ROWS / 32, WIN_WAVES = 8, WIN_GROUPS = 256;
+
+// Who has which keys on columns.  A key tile of the dense prefix sees all query tiles, `per` of them a share, and a wave has one share; the waves left over have the tiles behind
+// the prefix, which see one tile of the mask, in turn (with none left over, the last waves have one each besides).  So few shares that the longest wave has least.
+struct WindowWork { int shares, per; };
+inline WindowWork window_work(int tiles, int heavy, int mask_tile)
+{
+    WindowWork best = { 1, tiles };
+    int least = 1 << 30;
+    for (int want = 1; want <= tiles && heavy; ++want) {
+        const int per = (tiles + want - 1) / want, shares = (tiles + per - 1) / per, others = WIN_WAVES - heavy * shares, n = tiles - heavy, light = mask_tile < tiles ? mask_tile : tiles;
+        if (others < 0) break;
+        const int longest = n == 0 ? per : others == 0 ? per + light : per > (n + others - 1) / others * light ? per : (n + others - 1) / others * light;
+        if (longest < least) {
+            least = longest;
+            best = { shares, per };
+        }
+    }
+    return best;
+}
 
 template <int D>
 struct WinCfg {
@@ -44,7 +63,7 @@ __device__ __forceinline__ void store_direct(const f32x16 *acc, bf16 *row, bool 
 
 template <int D>
 __global__ void __launch_bounds__(64 * WIN_WAVES, 2)
-backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
+backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__restrict__ parts)
 {
     using C = BwdCfg<D, 1>;
     using W = WinCfg<D>;
@@ -56,8 +75,9 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
     const int heavy = min(P.n_pre << mb, tiles);
     const bool alive = wave < tiles;
     // this wave's work on columns: a tile behind the prefix, and a share of a tile of the prefix
-    const int want = heavy ? min(max(WIN_WAVES / heavy, 1), tiles) : 1, per = (tiles + want - 1) / want, shares = (tiles + per - 1) / per;
-    const int light = heavy + WIN_WAVES - 1 - wave, share = wave % shares, dense = wave / shares;       // (tiles; a light one >= tiles, a dense one >= heavy: none)
+    const int shares = work.shares, per = work.per, share = wave % shares, dense = wave / shares, others = WIN_WAVES - heavy * shares;
+    const int light = others == 0 ? heavy + WIN_WAVES - 1 - wave : wave >= WIN_WAVES - others ? heavy + wave - (WIN_WAVES - others) : tiles, step = others ? others : WIN_WAVES;
+    // (tiles; a light one >= tiles, a dense one >= heavy: none)
 
     f32x16 table = zero16();                                  // drel of table wave / DT, features 32 (wave % DT) ..
 
@@ -337,9 +357,10 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
 #pragma unroll
         for (int t = 0; t < C::DT; ++t) { dk[t] = zero16(); dv[t] = zero16(); }
 #pragma unroll 1
-        for (int pass = 0; pass < 2; ++pass) {
-            const int tile = pass ? dense : light, i0 = pass ? share * per : tile >> mb << mb, i1 = min(i0 + (pass ? per : 1 << mb), tiles);
-            if (tile >= (pass ? heavy : tiles)) continue;     // the same for the whole wave
+        for (int next = light;; next += step) {              // the tiles behind the prefix, then the share
+            const bool behind = next < tiles;
+            if (!behind && dense >= heavy) break;             // the same for the whole wave
+            const int tile = behind ? next : dense, i0 = behind ? tile >> mb << mb : share * per, i1 = min(i0 + (behind ? 1 << mb : per), tiles);
             const int kpos = tile * 32 + l32;
             if (tile != tile0) {                             // (keys past the end repeat the last one; their results are not stored)
                 const long from = ((long)grp * S + min(kpos, S - 1)) * P.row_stride + (long)head * D + half * 8;
@@ -391,12 +412,13 @@ backward_windows_kernel(BwdParams P, bool tables, float *__restrict__ parts)
             for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dk[dt][r] *= P.scale;
-            if (pass == 0 || shares == 1) {
+            if (behind || shares == 1) {
                 const int stored = tile * 32 + (lane_now() & 31);
                 const long to = ((long)grp * S + stored) * P.grad_stride + (long)head * D;
                 store_direct<D>(dk, P.dk + to, stored < S);
                 store_direct<D>(dv, P.dv + to, stored < S);
             }
+            if (!behind) break;
         }
         if (shares > 1 && heavy) {                           // the shares of a tile, added up in order
             __syncthreads();
