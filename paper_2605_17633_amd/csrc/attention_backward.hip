@@ -275,11 +275,12 @@ backward_prepare_kernel(BwdParams P, int blocks, int total)
 template <int D, int NT, bool LOCAL>
 struct RowStage {
     using C = BwdCfg<D, NT>;
-    static constexpr int KEYS = LOCAL ? 64 : 32;
+    static constexpr bool FULL = D == 80 && NT == 4;          // registers and LDS are short: dO in LDS, for which the stages are halved
+    static constexpr int KEYS = LOCAL && !FULL ? 64 : 32;
     static constexpr int KP = D * 2, EP = LOCAL ? 64 : C::EW * 2, TP = C::EW * 2;   // rows, in bytes
     static constexpr int K = 0, V = K + KEYS * KP, E = V + KEYS * KP, BYTES = E + KEYS * EP;
     static constexpr int T = 2 * BYTES, O = T + 4 * 32 * TP;
-    static constexpr bool KEEP = NT < 8;                      // a wave's dO stays in registers, else in LDS
+    static constexpr bool KEEP = NT < 8 && !(LOCAL && FULL);                      // a wave's dO stays in registers, else in LDS
     static constexpr int TOTAL = O + (KEEP ? 0 : 4 * 32 * C::VP * 2);
     static_assert(2 * BYTES <= 64 * 1024, "requests reach the first 64 KB");
 };
@@ -352,15 +353,23 @@ backward_rows_kernel(BwdParams P, int tiles)
     {
         _Float16 *u_row = reinterpret_cast<_Float16 *>(smem) + (wave * 32 + l32) * C::UP;
         constexpr int FIRST = 2 * C::WK;                     // the place of entry 0
+        bf16x8 ahead[C::KS];                                 // rows of the next product: asked for a product earlier
+        auto rows = [&](int tab, int m0) __attribute__((always_inline)) {
+            const bf16 *rp = (tab ? P.rel_w : P.rel_h) + (long)min(m0 + l32, nrel - 1) * D + half * 8;
+#pragma unroll
+            for (int ks = 0; ks < C::KS; ++ks) ahead[ks] = *reinterpret_cast<const bf16x8 *>(rp + ks * 16);
+        };
+        rows(0, 0);
 #pragma unroll
         for (int tab = 0; tab < 2; ++tab) {
             wave_lds_fence();
             _Float16 *to = u_row + (FIRST + w - 1 + (tab ? qrc >> 16 : qrc & 0xffff) - 4 * half);
             for (int m0 = 0; m0 < nrel; m0 += 32, to -= 32) {
-                const bf16 *rp = (tab ? P.rel_w : P.rel_h) + (long)min(m0 + l32, nrel - 1) * D + half * 8;
                 f32x16 u = zero16();
 #pragma unroll
-                for (int ks = 0; ks < C::KS; ++ks) u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(rp + ks * 16), qf[ks], u, 0, 0, 0);
+                for (int ks = 0; ks < C::KS; ++ks) u = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[ks], qf[ks], u, 0, 0, 0);
+                const bool more = m0 + 32 < nrel;
+                rows(more ? tab : 1, more ? m0 + 32 : 0);
                 mfma_settle();
 #pragma unroll
                 for (int r = 0; r < 16; ++r) to[-8 * (r >> 2) - (r & 3)] = (_Float16)(u[r] * P.inv_scale);
@@ -630,11 +639,17 @@ backward_rows_kernel(BwdParams P, int tiles)
 #pragma unroll
     for (int tab = 0; tab < 2; ++tab) {
         __syncthreads();
-        for (int i = tid; i < relrows * CH; i += 256) {
-            const int row = i / CH, c = i - row * CH;
-            u32x4 v = { 0, 0, 0, 0 };
-            if (row < nrel) v = *reinterpret_cast<const u32x4 *>((tab ? P.rel_w : P.rel_h) + (long)row * D + c * 8);
-            *reinterpret_cast<u32x4 *>(rel + row * C::VP + c * 8) = v;
+        constexpr int RELS = (2 * C::WK * CH + 255) / 256;
+        u32x4 rv[RELS];                                      // all asked for before the first is waited for
+#pragma unroll
+        for (int k = 0; k < RELS; ++k) {
+            const int i = tid + 256 * k, row = i / CH, c = i - row * CH;
+            rv[k] = *reinterpret_cast<const u32x4 *>((tab ? P.rel_w : P.rel_h) + (long)min(row, nrel - 1) * D + c * 8);
+        }
+#pragma unroll
+        for (int k = 0; k < RELS; ++k) {
+            const int i = tid + 256 * k, row = i / CH, c = i - row * CH;
+            if (row < relrows) *reinterpret_cast<u32x4 *>(rel + row * C::VP + c * 8) = row < nrel ? rv[k] : u32x4{ 0, 0, 0, 0 };
         }
         for (int i = 8 * half; i < relrows; i += 16) *reinterpret_cast<uint4 *>(mine + i) = make_uint4(0, 0, 0, 0);
         const int t0 = (tab ? qrc >> 16 : qrc & 0xffff) + w - 1;
@@ -653,6 +668,7 @@ backward_rows_kernel(BwdParams P, int tiles)
                 }
             if (part == 0) __syncthreads();
             else wave_lds_fence();
+#pragma unroll 2
             for (int t = 0; t < relrows / 16; ++t) {
                 const bf16x4 a = *reinterpret_cast<const bf16x4 *>(mine + 16 * t + 4 * half), b = *reinterpret_cast<const bf16x4 *>(mine + 16 * t + 8 + 4 * half);
                 const bf16x8 g8 = { a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3] };
@@ -1132,13 +1148,12 @@ int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w
     // orders that all groups share are the position-only ones, whose blocks of keys are patches of a grid of a power of two (28 x 28, where they are not: 67 us against 45);
     // those of one group alone scatter them
     const bool local = NT == 1 || (P.sigma_stride == 0 && (P.w & (P.w - 1)) == 0);
-    constexpr bool L = !(D == 80 && NT == 4);
     const int blocks = P.SP / 32, total = blocks * (P.sigma_stride ? P.n_gh / P.h : 1);
-    auto prepare = local && L ? backward_prepare_kernel<NT, true> : backward_prepare_kernel<NT, NT == 1>;
+    auto prepare = local ? backward_prepare_kernel<NT, true> : backward_prepare_kernel<NT, NT == 1>;
     hipLaunchKernelGGL(prepare, dim3(ssam_div_up(total, 4)), dim3(256), 0, st, P, blocks, total);
     SSAM_CHECK_LAUNCH();
-    auto rows = local ? backward_rows_kernel<D, NT, L> : backward_rows_kernel<D, NT, NT == 1>;
-    const size_t lds = local ? rows_lds_bytes<D, NT, L>(nrel) : rows_lds_bytes<D, NT, NT == 1>(nrel);
+    auto rows = local ? backward_rows_kernel<D, NT, true> : backward_rows_kernel<D, NT, NT == 1>;
+    const size_t lds = local ? rows_lds_bytes<D, NT, true>(nrel) : rows_lds_bytes<D, NT, NT == 1>(nrel);
     if (int rc = allow_lds(rows, lds); rc != SSAM_OK) return rc;
     if (int rc = allow_lds(backward_columns_kernel<D, NT>, columns_lds_bytes<D, NT>()); rc != SSAM_OK) return rc;
     hipLaunchKernelGGL(rows, dim3(grid), dim3(256), lds, st, P, tiles);
