@@ -74,9 +74,13 @@ def _check(name, rc):
 # The handle of the current device's current stream.  torch.cuda.current_stream() builds a Stream object around the same handle, 3.0 of the
 # 8.5 us that a call took on the host (0.35 this way): four dependent calls on one image's scores were bound by it, 33 us for 22 of kernels.
 if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):          # private names of torch
+    _device = torch._C._cuda_getDevice
+
     def _stream():
         return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
 else:
+    _device = torch.cuda.current_device
+
     def _stream():
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
@@ -543,14 +547,14 @@ def ssam_neck(x, w1, ln1_g, ln1_b, w2, ln2_g, ln2_b, g, eps=1e-6, out=None, work
 # ------------------------------------------------------------------ gradients
 def _one_device(**tensors):
     """Kernels run on the current device: a tensor that lies on another one is refused."""
-    here = torch.cuda.current_device()
+    here = _device()
     for name, t in tensors.items():
-        if t is not None and t.device.index != here:
+        if t is not None and t.get_device() != here:
             raise ValueError(f"{name}: on {t.device}, but the current device is cuda:{here}")
 
 
 def _shape(t, want, name):
-    if t is not None and tuple(t.shape) != tuple(want):
+    if t is not None and t.shape != tuple(want):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(want)}")
 
 
@@ -612,7 +616,7 @@ def ssam_ln_gather_backward(x, idx, idx_batch_stride, gamma, eps, dy, dx=None, a
     _shape(dx, x.shape, "dx")
     dgamma = dbeta = None
     if weight_grads:
-        dgamma, dbeta = (torch.empty(D, dtype=torch.float32, device=x.device) for _ in range(2))
+        dgamma, dbeta = x.new_empty(D, dtype=torch.float32), x.new_empty(D, dtype=torch.float32)
         if workspace is None:
             workspace = torch.empty(ssam_ln_gather_backward_workspace_bytes(B, Nout, D), dtype=torch.uint8, device=x.device)
     _one_device(x=x, idx=idx, gamma=gamma, dy=dy, dx=dx, workspace=workspace)
@@ -628,14 +632,15 @@ CHECKPOINT_COLUMNS = 64       # columns of a row that share a scale
 
 def _checkpoint(like, codes, scales):
     D = like.shape[-1]
-    lead = tuple(like.shape[:-1])
     if codes is None:
-        codes = torch.empty((*lead, D), dtype=torch.int8, device=like.device)
+        codes = torch.empty_like(like, dtype=torch.int8)
+    else:
+        _shape(codes, like.shape, "codes")
+    blocks = (*like.shape[:-1], -(-D // CHECKPOINT_COLUMNS))
     if scales is None:
-        scales = torch.empty((*lead, -(-D // CHECKPOINT_COLUMNS)), dtype=torch.float32, device=like.device)
-    _shape(codes, (*lead, D), "codes")
-    _shape(scales, (*lead, -(-D // CHECKPOINT_COLUMNS)), "scales")
-    _one_device(activation=like, codes=codes, scales=scales)
+        scales = like.new_empty(blocks, dtype=torch.float32)
+    else:
+        _shape(scales, blocks, "scales")
     return codes, scales, C.c_long(like.numel() // D if D else 0), C.c_int(D)
 
 
@@ -643,6 +648,7 @@ def ssam_checkpoint_store(x, codes=None, scales=None):
     """x [..., D] bf16 -> (codes [..., D] int8, scales [..., ceil(D/64)] fp32)."""
     px = _bf(x, "x")
     codes, scales, rows, D = _checkpoint(x, codes, scales)
+    _one_device(x=x, codes=codes, scales=scales)
     _check("ssam_checkpoint_store", lib().ssam_checkpoint_store(px, _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), rows, D, _stream()))
     return codes, scales
 
@@ -651,9 +657,10 @@ def ssam_checkpoint_restore(codes, scales, x=None):
     """The bf16 activation [..., D] that codes and scales hold."""
     pc, ps = _dev(codes, torch.int8, "codes"), _f32(scales, "scales")
     if x is None:
-        x = torch.empty(codes.shape, dtype=torch.bfloat16, device=codes.device)
+        x = torch.empty_like(codes, dtype=torch.bfloat16)
     px = _bf(x, "x")
     _, _, rows, D = _checkpoint(x, codes, scales)
+    _one_device(codes=codes, scales=scales, x=x)
     _check("ssam_checkpoint_restore", lib().ssam_checkpoint_restore(pc, ps, px, rows, D, _stream()))
     return x
 
@@ -663,10 +670,11 @@ def ssam_gelu_checkpoint(h, a=None, codes=None, scales=None):
     ph = _bf(h, "h")
     if a is None:
         a = torch.empty_like(h)
-    _shape(a, h.shape, "a")
+    else:
+        _shape(a, h.shape, "a")
     pa = _bf(a, "a")
     codes, scales, rows, D = _checkpoint(h, codes, scales)
-    _one_device(a=a)
+    _one_device(h=h, a=a, codes=codes, scales=scales)
     _check("ssam_gelu_checkpoint", lib().ssam_gelu_checkpoint(ph, pa, _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), rows, D, _stream()))
     return a, codes, scales
 
@@ -676,12 +684,14 @@ def ssam_gelu_backward(codes, scales, da, dh=None, a=None, activation=True):
     pc, ps, pd = _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), _bf(da, "da")
     if dh is None:
         dh = torch.empty_like(da)
-    if a is None and activation:
+    else:
+        _shape(dh, da.shape, "dh")
+    if a is not None:
+        _shape(a, da.shape, "a")
+    elif activation:
         a = torch.empty_like(da)
-    _shape(dh, da.shape, "dh")
-    _shape(a, da.shape, "a")
     _, _, rows, D = _checkpoint(da, codes, scales)
-    _one_device(dh=dh, a=a)
+    _one_device(codes=codes, scales=scales, da=da, dh=dh, a=a)
     _check("ssam_gelu_backward", lib().ssam_gelu_backward(pc, ps, pd, _bf(dh, "dh"), _bf(a, "a"), rows, D, _stream()))
     return dh, a
 
