@@ -468,12 +468,27 @@ backward_rows_kernel(BwdParams P, int tiles)
 #pragma unroll
         for (int r = 0; r < 8; ++r) g[s][r] = 0.f;
     float m = -INFINITY, l = 0.f;
+    // a block's slices are asked for a stage ahead: read where they are used they cost a trip to the cache a block
+    uint32_t ahead[St::KEYS / 32];
+    auto look = [&](int s) __attribute__((always_inline)) {
+        if constexpr (LOCAL && C::ES > 2)
+#pragma unroll
+            for (int b = 0; b < St::KEYS / 32; ++b) ahead[b] = blocks[min(stage_key(s) / 32 + b, P.SP / 32 - 1)];
+    };
     __syncthreads();
     load(0);
+    look(0);
     for (int s = 0; s < stages; ++s) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        uint32_t now[St::KEYS / 32] = {};
+        if constexpr (LOCAL && C::ES > 2)
+#pragma unroll
+            for (int b = 0; b < St::KEYS / 32; ++b) now[b] = __builtin_amdgcn_readfirstlane(ahead[b]);
         LDS_BARRIER();                                       // this stage has landed, and nobody reads the other buffers any more
-        if (s + 1 < stages) load(s + 1);
+        if (s + 1 < stages) {
+            load(s + 1);
+            look(s + 1);
+        }
         const int key0 = stage_key(s);
 #pragma unroll 1
         for (int b = 0; b < St::KEYS / 32; ++b) {
@@ -486,7 +501,7 @@ backward_rows_kernel(BwdParams P, int tiles)
             int rs = 0, cs = 0, rc = 0;
             bool two = true;
             if constexpr (LOCAL && C::ES > 2) {
-                const uint32_t slices = __builtin_amdgcn_readfirstlane(blocks[kb >> 5]);
+                const uint32_t slices = b == 0 ? now[0] : now[St::KEYS / 32 - 1];
                 two = slices != 0;
                 rs = slices & 0xff;
                 cs = slices >> 8 & 0xff;
