@@ -15,9 +15,9 @@
 //
 // Groups of at most 224 tokens have a kernel of their own (attention_backward_window.h).
 //
-// 64 x 64, density 0.4 in position order: 16 heads of 64, one image 218 us (rows 121, columns 93, tables 15, sums 7, join 7), 16 heads of 80, four images 938 (rows 575, columns 392,
-// tables 67): 0.33 and 0.38 PFLOP/s of the five products that a gradient cannot do without, of 1.16 that a large product reaches.  28 x 28, 16 heads of 64: 76 us; 50 x 50, content order,
-// two images, 12 heads of 64: 197.  Of a walk's time the matrix pipe is busy a quarter (rows) to two fifths (columns), the vector unit a third, LDS a third, one after the other: two waves to
+// 64 x 64, density 0.4 in position order: 16 heads of 64, one image 209 us (rows 116, columns 92, tables 15, sums 7, join 7), 16 heads of 80, four images 880 (rows 539, columns 392,
+// tables 67): 0.34 and 0.40 PFLOP/s of the five products that a gradient cannot do without, of 1.16 that a large product reaches.  28 x 28, 16 heads of 64: 78 us; 50 x 50, content order,
+// two images, 12 heads of 64: 192.  Of a walk's time the matrix pipe is busy a quarter (rows) to two fifths (columns), the vector unit a third, LDS a third, one after the other: two waves to
 // a SIMD, of which one could fill the other's gaps, wait 34 to 43 % of the time.
 //
 // The bias and its gradient are products with the 0/1 matrix E that has a one at every key's row and one at its column: scores
@@ -282,12 +282,12 @@ backward_prepare_kernel(BwdParams P, int blocks, int total)
 template <int D, int NT, bool LOCAL>
 struct RowStage {
     using C = BwdCfg<D, NT>;
-    static constexpr bool FULL = D == 80 && NT == 4;          // registers and LDS are short: dO in LDS, for which the stages are halved
+    static constexpr bool FULL = D == 80 && (NT == 2 || NT == 4);         // registers and LDS are short: dO in LDS, for which the stages are halved
     static constexpr int KEYS = LOCAL && !FULL ? 64 : 32;
     static constexpr int KP = D * 2, EP = LOCAL ? 64 : C::EW * 2, TP = C::EW * 2;   // rows, in bytes
     static constexpr int K = 0, V = K + KEYS * KP, E = V + KEYS * KP, BYTES = E + KEYS * EP;
     static constexpr int T = 2 * BYTES, O = T + 4 * 32 * TP;
-    static constexpr bool KEEP = NT < 8 && !(LOCAL && FULL);                      // a wave's dO stays in registers, else in LDS
+    static constexpr bool KEEP = NT < 8 && !(LOCAL && FULL);  // a wave's dO stays in registers, else in LDS
     static constexpr int TOTAL = O + (KEEP ? 0 : 4 * 32 * C::VP * 2);
     static_assert(2 * BYTES <= 64 * 1024, "requests reach the first 64 KB");
 };
@@ -567,6 +567,13 @@ backward_rows_kernel(BwdParams P, int tiles)
                 dp[r] = p * (dp[r] - delta);
             }
             const bf16x8 ds[2] = { half_of(dp, 0), half_of(dp, 1) };
+            // On grids of up to 32 x 32 G takes dS as the sum of two bf16, as in windows: of 28 x 28 dQ is off by 2.4e-3 of its norm instead of 2.5e-3 (larger grids: 2.4e-3 with one, and
+            // they would pay for it: two products a block of 18, or eight of 32)
+            constexpr bool FINE = NT <= 2;
+            bf16x8 lo[2];
+            if constexpr (FINE)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) lo[r >> 3][r & 7] = (bf16)(dp[r] - (float)ds[r >> 3][r & 7]);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -575,15 +582,27 @@ backward_rows_kernel(BwdParams P, int tiles)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int c = 0; c < NT; ++c) gt[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, t, c), ds[t], gt[c], 0, 0, 0);
+                    for (int c = 0; c < NT; ++c) {
+                        const bf16x8 one = et(smem, eat, t, c);
+                        gt[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one, ds[t], gt[c], 0, 0, 0);
+                        if constexpr (FINE) gt[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one, lo[t], gt[c], 0, 0, 0);
+                    }
             } else if constexpr (C::ES == 2) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) gt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, t, 0), ds[t], gt[0], 0, 0, 0);
+                for (int t = 0; t < 2; ++t) {
+                    const bf16x8 one = et(smem, eat, t, 0);
+                    gt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one, ds[t], gt[0], 0, 0, 0);
+                    gt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one, lo[t], gt[0], 0, 0, 0);
+                }
             } else {
                 // rows' slice in registers 0 to 7 of the product, columns' in 8 to 15
 #pragma unroll 1
                 for (int i = 0; i < (two ? 1 : C::ES); ++i) {
-                    bf16x8 some[2] = { ds[0], ds[1] };
+                    bf16x8 some[2] = { ds[0], ds[1] }, rest[2];
+                    if constexpr (FINE) {
+                        rest[0] = lo[0];
+                        rest[1] = lo[1];
+                    }
                     int to_r = rs, to_c = cs + C::ES / 2;
                     if (!two) {                              // dS of the keys in slice i
                         const bool is_row = i < C::ES / 2;
@@ -592,10 +611,18 @@ backward_rows_kernel(BwdParams P, int tiles)
                         to_r = is_row ? i : -1;
                         to_c = is_row ? -1 : i;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) some[r >> 3][r & 7] = keys >> (8 * (r >> 2) + (r & 3) + 4 * half) & 1 ? ds[r >> 3][r & 7] : (bf16)0.f;
+                        for (int r = 0; r < 16; ++r) {
+                            const bool in = keys >> (8 * (r >> 2) + (r & 3) + 4 * half) & 1;
+                            some[r >> 3][r & 7] = in ? ds[r >> 3][r & 7] : (bf16)0.f;
+                            if constexpr (FINE) rest[r >> 3][r & 7] = in ? lo[r >> 3][r & 7] : (bf16)0.f;
+                        }
                     }
                     f32x16 part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, 0, 0), some[0], zero16(), 0, 0, 0);
                     part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, 1, 0), some[1], part, 0, 0, 0);
+                    if constexpr (FINE) {
+                        part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, 0, 0), rest[0], part, 0, 0, 0);
+                        part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(et(smem, eat, 1, 0), rest[1], part, 0, 0, 0);
+                    }
                     mfma_settle();
 #pragma unroll
                     for (int k = 0; k < C::ES; ++k)
