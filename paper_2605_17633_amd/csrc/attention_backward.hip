@@ -44,7 +44,7 @@ struct BwdParams {
     long grad_stride;
     int S, w, h, n_gh;
     uint32_t per_w;              // 2^22 / w rounded up: a cell below 2^14 times it, over 2^22, is its row (the error, a cell / 2^22, is below 1 / w)
-    int mask_block, n_pre;       // tile of the mask, tiles of the dense prefix
+    int mask_block, n_pre;       // tile of the mask (grids: 128), tiles of the dense prefix
     float scale, scale_log2e, inv_scale, inv_scale_log2e;
     _Float16 *tab;               // [gh][SP][EW]: bias entries of a query, over the scale
     _Float16 *gsum;              // [gh][S][EW]: GH | GW over gunit; NULL: not wanted
@@ -788,7 +788,7 @@ __device__ __forceinline__ void walk_queries(const BwdParams &P, unsigned char *
             cs = __builtin_popcount(wanted & ((1u << cs) - 1));
         }
     }
-    const bool prefix = kb / P.mask_block < P.n_pre, alive = kb < S;
+    const bool alive = kb < S;
 
     // requests of a stage, 1 KB each, dealt out to the waves
     constexpr int CH = D / 8, TC = St::SLOTS * 2, NI = St::QUERIES * CH / 64, TI = St::QUERIES * TC / 64;
@@ -846,7 +846,7 @@ __device__ __forceinline__ void walk_queries(const BwdParams &P, unsigned char *
 #pragma unroll 1
         for (int b = 0; b < St::QUERIES / 32; ++b) {
             const int qb = q0 + 32 * b;
-            if (!alive || qb >= last || !(prefix || qb / P.mask_block == kb / P.mask_block)) continue;     // the same for the whole wave
+            if (!alive || qb >= last) continue;              // the same for the whole wave
             const int at = buf * St::BYTES + 32 * b * St::QP;
             // result rows are queries: register r <-> query 8 (r >> 2) + 4 half + (r & 3); scores begin at -log sum exp, dP at -delta
             f32x16 p, ds;
@@ -1209,9 +1209,9 @@ int launch_backward(const BwdParams &P, float *parts, bf16 *drel_h, bf16 *drel_w
     SSAM_CHECK_LAUNCH();
     ColWork work;
     work.gh8 = ssam_div_up(P.n_gh, 8);
-    work.heavy = ssam_div_up(min(P.n_pre * P.mask_block, P.S), 128);                // (windows: mask tiles are 32, a wave looks at its own)
+    work.heavy = min(P.n_pre, tiles);
     work.light = tiles - work.heavy;
-    work.splits = P.mask_block == 128 ? column_splits((long)work.heavy * P.n_gh, P.S) : 1;
+    work.splits = column_splits((long)work.heavy * P.n_gh, P.S);
     hipLaunchKernelGGL((backward_columns_kernel<D, NT>), dim3((unsigned)(8L * work.gh8 * (work.heavy * work.splits + work.light))), dim3(256),
                        (columns_lds_bytes<D, NT>()), st, P, work, parts);
     SSAM_CHECK_LAUNCH();
