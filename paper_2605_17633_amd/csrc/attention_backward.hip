@@ -45,7 +45,9 @@ struct BwdParams {
     int S, w, h, n_gh;
     uint32_t per_w;              // 2^22 / w rounded up: a cell below 2^14 times it, over 2^22, is its row (the error, a cell / 2^22, is below 1 / w)
     int mask_block, n_pre;       // tile of the mask (grids: 128), tiles of the dense prefix
-    float scale, scale_log2e, inv_scale, inv_scale_log2e;
+    float scale, scale_log2e, inv_scale, inv_scale_log2e;        // inv_scale: what turns a bias into an entry, 1 / (scale * 2^n); n = 0 on grids
+    uint32_t one;                // windows: 2^n in fp16, the ones of E
+    float over_one;              // and 1 over what that is read as bf16, 2^(8 n - 7)
     _Float16 *tab;               // [gh][SP][EW]: bias entries of a query, over the scale
     _Float16 *gsum;              // [gh][S][EW]: GH | GW over gunit; NULL: not wanted
     // of every order (one, or one a group; see backward_prepare_kernel)
@@ -239,11 +241,11 @@ struct Straight {
 };
 
 // entries of a slice of 16, the eight of a half-wave: a one (of fp16) at place i, if that is one of them
-__device__ __forceinline__ f16x8 ones(int i)
+__device__ __forceinline__ f16x8 ones(int i, uint32_t one = 0x3c00u)
 {
     u32x4 e;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) e[j] = i >> 1 == j ? (i & 1 ? 0x3c000000u : 0x3c00u) : 0u;
+    for (int j = 0; j < 4; ++j) e[j] = i >> 1 == j ? (i & 1 ? one << 16 : one) : 0u;
     return __builtin_bit_cast(f16x8, e);
 }
 
@@ -1279,7 +1281,7 @@ extern "C" int ssam_sparse_attention_backward(const void *q, const void *k, cons
     if ((long)w * w != S || row_stride < (long)h * d || row_stride % 8 != 0 || grad_stride < (long)h * d || grad_stride % 8 != 0) return SSAM_EINVAL;
     for (const void *p : { q, k, v, rel_h, rel_w, out, dout, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)drel_h, (const void *)drel_w, (const void *)workspace })
         if (!ssam_aligned16(p)) return SSAM_EINVAL;
-    // bias entries are held over the scale in fp16: up to 128 as a logit at the least of these, spaced by 2^-15 of one at the most
+    // bias entries are held over the scale in fp16: on grids up to 128 as a logit at the least of these, spaced by 2^-15 of one at the most
     if (scale < 0x1p-9f || scale > 0x1p9f) return SSAM_EUNSUPPORTED;
     if (mask_block == 32 ? S > 224 : mask_block != 128 || S > 16384) return SSAM_EUNSUPPORTED;
     if ((long)S * row_stride * 2 > 0x7fffffffL) return SSAM_EUNSUPPORTED;              // 32-bit offsets within a group
@@ -1305,7 +1307,11 @@ extern "C" int ssam_sparse_attention_backward(const void *q, const void *k, cons
     P.scale = scale;
     P.scale_log2e = scale * LOG2E;
     P.tab = (_Float16 *)(ws + at.tab);
-    P.inv_scale = 1.f / scale;
+    // the forward's bounds of the bias: where it has windows, a power of two keeps +-45400 and more (in the forward's groups of tiles of 128, n is 0 at these scales)
+    const int n = mask_block == 32 ? window_scale(scale).shift : 0;
+    P.one = 0x3c00u + ((uint32_t)n << 10);
+    P.over_one = ldexpf(1.f, 7 - 8 * n);
+    P.inv_scale = ldexpf(1.f / scale, -n);
     P.inv_scale_log2e = 1.f / P.scale_log2e;
     P.gsum = drel_h ? (_Float16 *)(ws + at.gsum) : nullptr;
     P.gunit = (float *)(ws + at.gunit);

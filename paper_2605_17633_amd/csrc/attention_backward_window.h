@@ -188,7 +188,7 @@ backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__rest
             wave_lds_fence();
             // E: a half-wave has the row's 16 entries, the other one the column's
 #pragma unroll
-            for (int c = 0; c < 2; ++c) *reinterpret_cast<f16x8 *>(mine + ((2 * half + c) ^ swizzle<EC>(l32)) * 16) = ones((half ? col : row) - 8 * c);
+            for (int c = 0; c < 2; ++c) *reinterpret_cast<f16x8 *>(mine + ((2 * half + c) ^ swizzle<EC>(l32)) * 16) = ones((half ? col : row) - 8 * c, P.one);
         }
         __syncthreads();
         const Transposed<CH> ft(lane);
@@ -300,7 +300,7 @@ backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__rest
             for (int r = 0; r < 16; ++r) {
                 // (entries from w on are zeros: they go to positions that are none, below the first one's or, from the front of the row, to its end)
                 const int y = 8 * (r >> 2 & 1) + 4 * half + (r & 3), at = 32 * (r >> 3) + (((r >> 3 ? col : row) + w - 1 - y) & 31);
-                const float x = gt[r] * (inv * 128.f);
+                const float x = gt[r] * (inv * P.over_one);
                 const bf16 hi = (bf16)x;
                 bf16 *to = reinterpret_cast<bf16 *>(mine + ((at >> 3) ^ gsw) * 16) + (at & 7);
                 *to = hi;
@@ -382,7 +382,7 @@ backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__rest
                 }
             }
             const int krc = row_col(P.sigma + (long)grp * P.sigma_stride, kpos, P);
-            const f16x8 er = ones((krc & 0xffff) - 8 * half), ec = ones((krc >> 16) - 8 * half);
+            const f16x8 er = ones((krc & 0xffff) - 8 * half, P.one), ec = ones((krc >> 16) - 8 * half, P.one);
 #pragma unroll
             for (int t = 0; t < C::DT; ++t) { dk[t] = zero16(); dv[t] = zero16(); }
 #pragma unroll 1

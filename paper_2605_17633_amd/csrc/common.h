@@ -66,6 +66,24 @@ static inline int ssam_prefix_tiles(int T, double r)
     return (int)n;
 }
 
+// Bias entries of attention in windows: a bias over scale * 2^n, which meets a one of 2^n on its way into a score.  An entry of 1 is
+// scale * 2^n * log2 e units of a logit in powers of two, by the choice of n at least 1 (the range of such units: +-45400 as a logit) and below
+// 512 (the spacing of the smallest entries is then 2^-15 of one; with n = 0 at a scale of 1e6 a bias of 0.01 was 0), and n is 0 where it can
+// be, from a scale of 0.7 to 350.  Ones of fp16 hold 2^-14 to 2^15; past those, below a scale of 2e-5 and above 5e6, the rest goes into the
+// queries, as a power of two that rounds nothing.
+struct WindowScale { int shift, q_exp; };
+static inline WindowScale window_scale(float scale)
+{
+    const double unit = (double)scale * 1.4426950408889634;
+    int e, n = 0;
+    if (!(unit < HUGE_VAL)) return { 0, 0 };
+    frexp(unit, &e);                       // unit = 2^(e - 1) up to 2^e
+    if (e < 1) n = 1 - e;
+    else if (e > 9) n = 9 - e;
+    const int shift = n < -14 ? -14 : n > 15 ? 15 : n;
+    return { shift, shift - n };
+}
+
 __device__ __forceinline__ float bf16_bits_to_float(uint32_t hi16) { return __uint_as_float(hi16 << 16); }
 
 // 8 bf16 packed in a uint4 -> 8 floats
