@@ -1161,7 +1161,11 @@ inline BwdWorkspace workspace_layout(int groups, int S, int w, int h, int d)
 {
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     const size_t rows = (size_t)groups * h * ((S + 31) / 32 * 32), entries = rows * 32 * entry_tiles(w) * 2;
-    BwdWorkspace o;
+    BwdWorkspace o = {};
+    if (S <= WIN_ROWS) {                                     // sums of the tables' gradients alone: all else stays in LDS
+        o.total = (size_t)window_groups((long)groups * h) * 2 * 32 * d * 4;
+        return o;
+    }
     o.zeros = 0;
     o.tab = 1024;
     o.gsum = o.tab + up(entries + 32 * 64 * entry_tiles(w));                        // (the last stage reads up to 32 rows past the end)
@@ -1178,8 +1182,7 @@ inline BwdWorkspace workspace_layout(int groups, int S, int w, int h, int d)
     const size_t tables = (size_t)2 * w * table_slices(w, (long)groups * h) * 16 * entry_tiles(w) * d * 4;
     const long tiles = (long)groups * h * ssam_div_up(S, 128), slots = tiles * ssam_div_up(S, 256);
     const size_t columns = S <= 256 ? 0 : (size_t)(slots < COL_SLOTS ? slots : COL_SLOTS) * 128 * 2 * d * 4;
-    const size_t windows = S > WIN_ROWS ? 0 : (size_t)window_groups((long)groups * h) * 2 * 32 * d * 4, most = tables > columns ? tables : columns;
-    o.total = o.parts + up(most > windows ? most : windows);
+    o.total = o.parts + up(tables > columns ? tables : columns);
     return o;
 }
 
