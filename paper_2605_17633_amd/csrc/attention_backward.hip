@@ -1287,9 +1287,10 @@ extern "C" int ssam_sparse_attention_backward(const void *q, const void *k, cons
     // bias entries are held over the scale in fp16: on grids up to 128 as a logit at the least of these, spaced by 2^-15 of one at the most
     if (scale < 0x1p-9f || scale > 0x1p9f) return SSAM_EUNSUPPORTED;
     if (mask_block == 32 ? S > 224 : mask_block != 128 || S > 16384) return SSAM_EUNSUPPORTED;
-    if ((long)S * row_stride * 2 > 0x7fffffffL) return SSAM_EUNSUPPORTED;              // 32-bit offsets within a group
     if (d != 16 && d != 32 && d != 64 && d != 80) return SSAM_EUNSUPPORTED;
-    if ((long)groups * h > 0x7ffffff0L || (long)ssam_div_up(S, 128) * ((long)groups * h + 7) > 0x7fffffffL / 256) return SSAM_EUNSUPPORTED;
+    if ((long)groups * h > 0x7ffffff0L) return SSAM_EUNSUPPORTED;
+    // grids: 32-bit offsets within a group, a workgroup a tile of a (group, head)
+    if (S > WIN_ROWS && ((long)S * row_stride * 2 > 0x7fffffffL || (long)ssam_div_up(S, 128) * ((long)groups * h + 7) > 0x7fffffffL / 256)) return SSAM_EUNSUPPORTED;
     const BwdWorkspace at = workspace_layout(groups, S, w, h, d);
     if (workspace_bytes < at.total) return SSAM_EWORKSPACE;
     unsigned char *ws = (unsigned char *)workspace;
