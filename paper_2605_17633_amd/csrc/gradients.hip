@@ -224,7 +224,11 @@ __device__ __forceinline__ Quantised quantise_block(const uint4 &v)
     if (top >= 0x7f80u) return r;
     const float most = bf16_bits_to_float(top);
     r.scale = fmaxf(most / 127.f, 0x1p-126f);
-    const float inv = top ? fminf(127.f / most, 0x1p126f) : 0.f;
+    // 127 / most, rounded up.  Half of the largest value is a tie for every block (63.5: 64), and with a factor that is too small by its rounding it came out as 63.  (Other ties need a
+    // largest value of 127 times a power of two, whose factor is exact; and quotients that are no ties are 7e-6 and more from one.)
+    float inv = 127.f / most;
+    if (fmaf(inv, most, -127.f) < 0.f) inv = __uint_as_float(__float_as_uint(inv) + 1u);
+    inv = top ? fminf(inv, 0x1p126f) : 0.f;
     float f[8];
     unpack_bf16x8(v, f);
     int c[8];
