@@ -87,14 +87,6 @@ __device__ __forceinline__ void set_ones_columns(bf16 *Vs, int rows, int tid, in
     }
 }
 
-// LDS is in order per wave: this keeps the compiler from reordering what its lanes exchange through it
-__device__ __forceinline__ void wave_lds_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // Per-wave softmax/output state for 32 queries (one per lane pair l, l^32).
 template <int D>
 struct WaveState {
@@ -139,8 +131,6 @@ inline int bias_shift(float scale)
     while (n < 15 && ldexpf(65504.f / 128.f * scale, n) < 1.f) ++n;
     return n;
 }
-// bit 23 of the mode register: fp16 results past the range are clamped instead of rounded to infinity
-__device__ __forceinline__ void clamp_fp16() { __builtin_amdgcn_s_setreg(1 | 23 << 6 | (1 - 1) << 11, 1); }
 
 __host__ __device__ inline int glb_tstr(int w) { return 4 * ((w + 1) >> 1) + 4; }
 // Entries per table of the operand form (AttnPipe), 0: look-ups.  Two images of 50 x 50, d = 80: 111 us by look-up, 88 by dense operands (sparse

@@ -72,9 +72,6 @@ struct BwdCfg {
     static constexpr int UP = 4 * WK + 8;                    // of products with a table at the entries' places
 };
 
-// bit 23 of the mode register: fp16 results past the range are clamped instead of rounded to infinity (which would make NaNs of the zeros of E)
-__device__ __forceinline__ void clamp_fp16() { __builtin_amdgcn_s_setreg(1 | 23 << 6 | (1 - 1) << 11, 1); }
-
 // row | column << 16 of a position's cell (positions past the end: the last one's; cells are held to the grid)
 __device__ __forceinline__ int row_col(const int32_t *sigma, int at, const BwdParams &P)
 {
@@ -89,13 +86,6 @@ __device__ __forceinline__ void mfma_settle()
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-}
-
-__device__ __forceinline__ void wave_lds_fence()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 __device__ __forceinline__ f32x16 zero16()
@@ -411,6 +401,7 @@ backward_rows_kernel(BwdParams P, int tiles)
     auto upstream = [&](int ks) { return St::KEEP ? of[ks] : *reinterpret_cast<const bf16x8 *>(os + ks * 16); };
 
     // stages of keys: the dense prefix, then (where a wave has a diagonal tile behind it) the workgroup's own 128
+    // (A mask tile is 128 here.  Written as the constant, so that the division goes, 64 features on 32 x 32 and 80 on grids up to 64 x 64 in scattering orders spill two registers and one.)
     const int pre = min(P.n_pre * P.mask_block, S), pre_stages = (pre + St::KEYS - 1) / St::KEYS;
     const int own = (q0 + wave * 32) / P.mask_block;                                  // mask tile of the wave's queries
     const bool any_diagonal = min(q0 + 127, S - 1) / P.mask_block >= P.n_pre;
@@ -719,7 +710,6 @@ backward_rows_kernel(BwdParams P, int tiles)
                 }
             if (part == 0) __syncthreads();
             else wave_lds_fence();
-#pragma unroll 2
             for (int t = 0; t < relrows / 16; ++t) {
                 const bf16x4 a = *reinterpret_cast<const bf16x4 *>(mine + 16 * t + 4 * half), b = *reinterpret_cast<const bf16x4 *>(mine + 16 * t + 8 + 4 * half);
                 const bf16x8 g8 = { a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3] };
@@ -1117,17 +1107,7 @@ backward_table_sums_kernel(const float4 *__restrict__ parts, int w, int WK, int 
         const float4 v = parts[(WINDOWS ? ((long)i * 2 + tab) * 32 + t : (((long)tab * w + R) * slices + i % slices) * WK + y) * quads + min(quad, quads - 1)];
         a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
     }
-    lds[threadIdx.x] = a;
-    __syncthreads();
-#pragma unroll
-    for (int half = 16; half > 0; half >>= 1) {
-        if (share < half) {
-            const float4 v = lds[threadIdx.x + half * 8];
-            a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
-            lds[threadIdx.x] = a;
-        }
-        __syncthreads();
-    }
+    a = sum_of_shares(a, lds);
     if (share == 0 && in) *reinterpret_cast<uint2 *>((tab ? drel_w : drel_h) + (long)t * D + quad * 4) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
 }
 

@@ -92,7 +92,7 @@ backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__rest
         if (gh >= P.n_gh) break;                             // the same for the whole workgroup
         const int grp = gh / P.h, head = gh - grp * P.h;
         const int lane = lane_now(), tid = wave * 64 + lane, l32 = lane & 31, half = lane >> 5, pos = wave * 32 + l32;
-        const int esw = swizzle<EC>(l32) ^ half, fsw = swizzle<CH>(l32) ^ half;
+        const int esw = swizzle<EC>(l32) ^ half;
         const bf16 *rel_h = P.rel_h, *rel_w = P.rel_w;
         asm volatile("" : "+s"(rel_h), "+s"(rel_w));           // (read again for every (group, head): kept, their rows would take 40 registers)
         const int rc = row_col(P.sigma + (long)grp * P.sigma_stride, pos, P), row = rc & 0xffff, col = rc >> 16;

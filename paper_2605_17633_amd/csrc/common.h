@@ -108,11 +108,40 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float *f)
                       pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
 }
 
+// LDS is in order per wave: this keeps the compiler from reordering what its lanes exchange through it
+__device__ __forceinline__ void wave_lds_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// bit 23 of the mode register: fp16 results past the range are clamped instead of rounded to infinity (which would make NaNs of the zeros of a 0/1 matrix)
+__device__ __forceinline__ void clamp_fp16() { __builtin_amdgcn_s_setreg(1 | 23 << 6 | (1 - 1) << 11, 1); }
+
 __device__ __forceinline__ float wave_sum(float v)
 {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     return v;
+}
+
+// Sum over the 32 shares of a workgroup of 256 threads, thread = share * 8 + column: each column's is what share 0 gets.  In a fixed order.
+__device__ __forceinline__ float4 sum_of_shares(float4 a, float4 *lds)
+{
+    const int share = threadIdx.x >> 3;
+    lds[threadIdx.x] = a;
+    __syncthreads();
+#pragma unroll
+    for (int half = 16; half > 0; half >>= 1) {
+        if (share < half) {
+            const float4 t = lds[threadIdx.x + half * 8];
+            a.x += t.x; a.y += t.y; a.z += t.z; a.w += t.w;
+            lds[threadIdx.x] = a;
+        }
+        __syncthreads();
+    }
+    return a;
 }
 
 // one padding row (see PadFill): a wave, 16 bytes per lane.  A launch of its own took 5 us of every unfolded block with padding
@@ -182,6 +211,15 @@ __device__ __forceinline__ float2 gemm_row_stats(const float2 *row, int slots, i
     return make_float2(inv, -inv * mean);
 }
 
+// (a1 + ... + a5 u^4) / 2 of the rational approximation below: u poly(u) exp(-x^2) is half of erfc(x)
+__device__ __forceinline__ float half_erfc_poly(float u)
+{
+    float poly = fmaf(0.5f * 1.061405429f, u, -0.5f * 1.453152027f);
+    poly = fmaf(poly, u, 0.5f * 1.421413741f);
+    poly = fmaf(poly, u, -0.5f * 0.284496736f);
+    return fmaf(poly, u, 0.5f * 0.254829592f);
+}
+
 // erf GELU, 0.5 t (1 + erf(t / sqrt 2)) = max(t, 0) - 0.5 |t| erfc(|t| / sqrt 2).  erfc by the rational approximation 7.1.26 of
 // Abramowitz & Stegun, erfc(x) = (a1 u + ... + a5 u^5) exp(-x^2), u = 1 / (1 + p x) for x >= 0; absolute error below
 // 1.5e-7, far under the bf16 rounding of the stored activation.  One reciprocal and one exp2 per element, eleven full-rate
@@ -194,10 +232,7 @@ __device__ __forceinline__ float gelu_erf(float t)
 {
     const float a = fabsf(t);
     const float u = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752440f, a, 1.0f));
-    float poly = fmaf(0.5f * 1.061405429f, u, -0.5f * 1.453152027f);
-    poly = fmaf(poly, u, 0.5f * 1.421413741f);
-    poly = fmaf(poly, u, -0.5f * 0.284496736f);
-    poly = fmaf(poly, u, 0.5f * 0.254829592f);
+    const float poly = half_erfc_poly(u);
     const float s = a * 0.84932180028801904272f;               // sqrt(log2(e) / 2)
     const float e = __builtin_amdgcn_exp2f(-s * s);
     float au;

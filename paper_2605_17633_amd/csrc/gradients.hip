@@ -144,17 +144,7 @@ ln_weight_sums_kernel(const float4 *__restrict__ parts, int n, int D, float *__r
         const float4 t = parts[(long)r * quads + min(col, quads - 1)];
         a.x += t.x; a.y += t.y; a.z += t.z; a.w += t.w;
     }
-    lds[threadIdx.x] = a;
-    __syncthreads();
-#pragma unroll
-    for (int half = 16; half > 0; half >>= 1) {
-        if (slice < half) {
-            const float4 t = lds[threadIdx.x + half * 8];
-            a.x += t.x; a.y += t.y; a.z += t.z; a.w += t.w;
-            lds[threadIdx.x] = a;
-        }
-        __syncthreads();
-    }
+    a = sum_of_shares(a, lds);
     if (slice == 0 && in) *reinterpret_cast<float4 *>(4 * col < D ? dgamma + 4 * col : dbeta + 4 * col - D) = a;
 }
 
@@ -250,10 +240,7 @@ __device__ __forceinline__ void gelu_slope(float t, float &gelu, float &slope)
 {
     const float a = fabsf(t);
     const float u = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752440f, a, 1.0f));
-    float poly = fmaf(0.5f * 1.061405429f, u, -0.5f * 1.453152027f);
-    poly = fmaf(poly, u, 0.5f * 1.421413741f);
-    poly = fmaf(poly, u, -0.5f * 0.284496736f);
-    poly = fmaf(poly, u, 0.5f * 0.254829592f);
+    const float poly = half_erfc_poly(u);
     const float s = a * 0.84932180028801904272f;               // sqrt(log2(e) / 2)
     const float e = __builtin_amdgcn_exp2f(-s * s);
     const float tail = u * poly * e;                            // 1 - Phi(|t|)
