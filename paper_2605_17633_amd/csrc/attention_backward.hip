@@ -230,6 +230,14 @@ struct Straight {
     }
 };
 
+// Bias entries past the range of fp16 (infinities by the conversion) are bounded to it: with an infinity the zeros of E would make NaNs of a query's whole row.  NaN stays NaN.  (The mode
+// bit that clamps conversions, which the forward's kernels set, is no choice here: with it the matrix instructions take NaN for 0 and infinities for the largest number, so that a
+// gradient that is not finite would come back as an ordinary one.)
+__device__ __forceinline__ f16x8 bounded(f16x8 v)
+{
+    return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, (f16x8)(_Float16)-65504.f), (f16x8)(_Float16)65504.f);
+}
+
 // entries of a slice of 16, the eight of a half-wave: a one (of fp16) at place i, if that is one of them
 __device__ __forceinline__ f16x8 ones(int i, uint32_t one = 0x3c00u)
 {
@@ -307,7 +315,6 @@ backward_rows_kernel(BwdParams P, int tiles)
     // the tiles of one (group, head) run on one XCD (workgroup b sits on XCD b & 7), whose L2 then serves the re-reads of its K and V
     const int tile = (blockIdx.x >> 3) % tiles, gh = ((blockIdx.x >> 3) / tiles) * 8 + (blockIdx.x & 7);
     if (gh >= P.n_gh) return;
-    clamp_fp16();
     const int grp = gh / P.h, head = gh - grp * P.h;
     const int S = P.S, w = P.w, nrel = 2 * w - 1;
     const int q0 = tile * 128, qpos = q0 + wave * 32 + l32;
@@ -379,7 +386,7 @@ backward_rows_kernel(BwdParams P, int tiles)
                 f16x8 v = *reinterpret_cast<const f16x8 *>(u_row + FIRST + 16 * c + 8 * half);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = 16 * c + 8 * half + e < w ? v[e] : (_Float16)0.f;
-                bt[tab * C::ES / 2 + c] = v;
+                bt[tab * C::ES / 2 + c] = bounded(v);
             }
         }
     }

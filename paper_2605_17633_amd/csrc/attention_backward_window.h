@@ -74,7 +74,6 @@ backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__rest
     constexpr int CH = D / 8, EC = W::EB / 16;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    clamp_fp16();
     const int S = P.S, w = P.w, nrel = 2 * w - 1, tiles = (S + 31) / 32, mb = P.mask_block == 128 ? 2 : 0;                        // (log of a mask tile's 32s)
     const int heavy = min(P.n_pre << mb, tiles);
     const bool alive = wave < tiles;
@@ -184,6 +183,7 @@ backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__rest
                     const _Float16 x = *reinterpret_cast<const _Float16 *>(mine + ((t >> 2) ^ usw) * 8 + (t & 3) * 2);
                     bt[tab][e] = 8 * half + e < w ? x : (_Float16)0.f;
                 }
+                bt[tab] = bounded(bt[tab]);
             }
             wave_lds_fence();
             // E: a half-wave has the row's 16 entries, the other one the column's
@@ -298,9 +298,9 @@ backward_windows_kernel(BwdParams P, WindowWork work, bool tables, float *__rest
             wave_lds_fence();
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                // (entries from w on are zeros: they go to positions that are none, below the first one's or, from the front of the row, to its end)
+                // (entries from w on are none: as zeros they go to positions below the first one's or, from the front of the row, to its end)
                 const int y = 8 * (r >> 2 & 1) + 4 * half + (r & 3), at = 32 * (r >> 3) + (((r >> 3 ? col : row) + w - 1 - y) & 31);
-                const float x = gt[r] * (inv * P.over_one);
+                const float x = y < w ? gt[r] * (inv * P.over_one) : 0.f;
                 const bf16 hi = (bf16)x;
                 bf16 *to = reinterpret_cast<bf16 *>(mine + ((at >> 3) ^ gsw) * 16) + (at & 7);
                 *to = hi;
