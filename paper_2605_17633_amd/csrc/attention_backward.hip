@@ -15,10 +15,11 @@
 //
 // Groups of at most 224 tokens have a kernel of their own (attention_backward_window.h).
 //
-// 64 x 64, density 0.4 in position order: 16 heads of 64, one image 209 us (rows 116, columns 92, tables 15, sums 7, join 7), 16 heads of 80, four images 880 (rows 539, columns 392,
-// tables 67): 0.34 and 0.40 PFLOP/s of the five products that a gradient cannot do without, of 1.16 that a large product reaches.  28 x 28, 16 heads of 64: 78 us; 50 x 50, content order,
-// two images, 12 heads of 64: 192.  Of a walk's time the matrix pipe is busy a quarter (rows) to two fifths (columns), the vector unit a third, LDS a third, one after the other: two waves to
-// a SIMD, of which one could fill the other's gaps, wait 34 to 43 % of the time.
+// 64 x 64, density 0.4 in position order: 16 heads of 64, one image 208 us, 16 heads of 80, four images 876: 0.34 and 0.41 PFLOP/s of the five products that a gradient cannot do
+// without, of 1.16 that a large product reaches.  28 x 28, 12 heads of 64: 78 us; 50 x 50, content order, two images, 12 heads of 64: 191; 128 x 128, density 0.1, 16 heads of 64: 1665, in
+// content order 2014 (one wave to a SIMD).  Under the tracer, where launches take longer (239 and 937 us together), rows are 116 and 492, columns 90 and 368, tables with their sums 22 and 73, the
+// join 6.  Of a walk's time the matrix pipe is busy a quarter (rows) to two fifths (columns), the vector unit and LDS over a third each, one after the other: two waves to a SIMD,
+// of which one could fill the other's gaps, wait 36 % of the time.
 //
 // The bias and its gradient are products with the 0/1 matrix E that has a one at every key's row and one at its column: scores
 // take E T (T the entries of a query, fp16, over the scale), G is E^T dS.  E sits behind the keys' features in LDS, [key][K | E], so that one set

@@ -7,7 +7,7 @@
 //   columns  every active (query tile, key tile) once more with P from the statistics.  Keys of the dense prefix see all queries: their query tiles are dealt out to several waves,
 //            whose sums are added through LDS in order; the others see one tile of the mask
 // Why eight waves and all of LDS: the features of a (group, head) of 14 x 14 x 80 are 126 KB, so one workgroup has the CU, and two waves to a SIMD have 256 registers each.
-// 1600 (group, head) of 14 x 14 x 80 (four images, 16 heads, density 0.5) take 224 us, 400 of 64 features 52; in rows, columns and tables as for grids they took 336 and 66.  A (group, head)
+// 1600 (group, head) of 14 x 14 x 80 (four images, 16 heads, density 0.5) take 223 us, 300 of 64 features 52; in rows, columns and tables as for grids they took 336 and 66.  A (group, head)
 // is a chain of phases between barriers, 32 us of the former: 13 until its rows are there (250 MB read and 150 written at 1.8 TB/s over the whole), 3 bias entries, 4 to 6 rows, 3 G,
 // 4 dQ and tables, 4 to 6 columns; the matrix pipe is busy 15 % of the time.
 // The space of K and V holds G (as the sum of two bf16) and the relative positions' features once the rows are done; that of E then holds the bias entries T.

@@ -248,8 +248,8 @@ __device__ __forceinline__ void gelu_slope(float t, float &gelu, float &slope)
     slope = fmaf(t * 0.39894228040143267794f, e, t < 0.f ? tail : 1.f - tail);
 }
 
-// Bound by HBM: 32768 x 1280 stored in 22 us and restored in 20 (128 MB each, 5.8 and 6.4 TB/s: the codes are still in the cache); GELU of 13104 x 5120 63 us forward and 88 backward
-// (814 MB together, 5.4 TB/s).  Small ones cost what their launches do, 3 to 4 us, and twice that on the host.
+// Bound by HBM: 32768 x 1280 stored in 21 us and restored in 20 (128 MB each, 6.1 and 6.4 TB/s: the codes are still in the cache); GELU of 13104 x 5120 64 to 72 us forward and 90 backward,
+// 150 both (814 MB together, 5.4 TB/s).  Small ones cost what their launches do, 3 to 4 us, and twice that on the host.
 enum CkptOp { CKPT_STORE, CKPT_RESTORE, CKPT_GELU, CKPT_GELU_BACKWARD };
 
 // A thread has the slots i and i + half of the launch: both are requested before the first is used, or anything stored (out may be in).
