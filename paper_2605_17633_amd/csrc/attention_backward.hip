@@ -23,7 +23,7 @@
 //
 // The bias and its gradient are products with the 0/1 matrix E that has a one at every key's row and one at its column: scores
 // take E T (T the entries of a query, fp16, over the scale), G is E^T dS.  E sits behind the keys' features in LDS, [key][K | E], so that one set
-// of transposing reads gives K^T and E^T.  Its ones are 0x3c00: 1 in fp16, 2^-7 in bf16, which G is multiplied by at the end.
+// of transposing reads gives K^T and E^T.  Its ones are 0x3c00: 1 in fp16, 2^-7 in bf16, which G is multiplied by at the end (in windows 2^n and 2^(8 n - 7)).
 // Operand layouts of v_mfma_f32_32x32x16 and of the transposing read are those of the forward kernels.
 #include "common.h"
 
@@ -48,7 +48,7 @@ struct BwdParams {
     int mask_block, n_pre;       // tile of the mask (grids: 128), tiles of the dense prefix
     float scale, scale_log2e, inv_scale, inv_scale_log2e;        // inv_scale: what turns a bias into an entry, 1 / (scale * 2^n); n = 0 on grids
     uint32_t one;                // windows: 2^n in fp16, the ones of E
-    float over_one;              // and 1 over what that is read as bf16, 2^(8 n - 7)
+    float over_one;              // and 1 over what that is as bf16, 2^(8 n - 7)
     _Float16 *tab;               // [gh][SP][EW]: bias entries of a query, over the scale
     _Float16 *gsum;              // [gh][S][EW]: GH | GW over gunit; NULL: not wanted
     // of every order (one, or one a group; see backward_prepare_kernel)
