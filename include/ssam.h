@@ -439,9 +439,10 @@ int ssam_neck(const void *x, const void *w1, const float *ln1_g, const float *ln
  * head), of 256 at most; above about 4 bytes * 32, 64, 128 or 256, the next multiple from 2w, per query and head).  Sums
  * are fp32, probabilities and their gradients bf16 where they are multiplied, bias entries fp16 over the scale and a power
  * of two (bounded as in the forward call: windows, mask_block 32, to +-45400 or more, global to +-65504 * scale, 128 or
- * more); no atomics: the same inputs give the same bits.  What is not finite comes through: a query's in dout or out to
- * its dQ, the dK and dV of the keys that it sees and the tables' gradients at the positions of those.  Built for the sizes
- * of the forward call (w <= 128, d in {16, 32, 64, 80}) and scales of 1/512 to 512, else SSAM_EUNSUPPORTED. */
+ * more); no atomics: the same inputs give the same bits.  What is not finite comes through: a query's in dout or, dV
+ * aside, in out to its dQ, the dK and dV of the keys that it sees and the tables' gradients at the positions of those.
+ * Built for the sizes of the forward call (w <= 128, d in {16, 32, 64, 80}) and scales of 1/512 to 512, else
+ * SSAM_EUNSUPPORTED. */
 size_t ssam_sparse_attention_backward_workspace_bytes(int groups, int S, int w, int h, int d);
 int ssam_sparse_attention_backward(const void *q, const void *k, const void *v, long row_stride,
                                    const void *rel_h, const void *rel_w, const int32_t *sigma,

@@ -70,6 +70,31 @@ def test_a_gradient_that_is_not_finite(case, value):
         assert torch.equal(a[beside], b[beside])
 
 
+@pytest.mark.parametrize("case", [(2, 14, 2, 80, 32, 0.4, "content", False), (1, 32, 2, 64, 128, 0.4, "position", False), (1, 50, 1, 80, 128, 0.3, "content", False)])
+def test_a_result_or_a_key_that_is_not_finite(case):
+    """NaN in out of one query: its delta, so all of its dS; dV, in which out is not, keeps its bits.  NaN in a key behind the prefix: P of the queries of its tile, and so their dQ, and dK and dV
+    of the keys that they see; no other query's dQ."""
+    announce("sparse_attention_backward result or key not finite", case)
+    groups, w, h, d, tile, r = case[:6]
+    S = w * w
+    (qkv, rel, sigma, _, dout, out), want = T.run(case, seed=66)
+    i = S - 2
+    t = torch.arange(S, device=DEV) // tile
+    seen = (t < R.prefix(S, tile, r)) | (t == t[i])
+    bad = out.clone()
+    bad[(groups - 1) * S + i, (h - 1) * d] = math.nan
+    got = B.ssam_sparse_attention_backward(qkv, *rel, sigma, w, tile, r, bad, dout)[0]
+    assert torch.equal(got[:, :, 2], want[0][:, :, 2])
+    assert bool(got[-1, i, 0, -1].isnan().all()) and bool(got[-1, seen, 1, -1].isnan().all())
+    assert int(got[:, :, :2].isnan().sum()) == d * (1 + int(seen.sum()))
+    keys = qkv.clone()
+    keys[-1, i, 1, -1, 1] = math.nan
+    got = B.ssam_sparse_attention_backward(keys, *rel, sigma, w, tile, r, out, dout)[0]
+    same = t == t[i]
+    assert bool(got[-1, same, 0, -1].isnan().all()) and int(got[:, :, 0].isnan().sum()) == d * int(same.sum())
+    assert bool(got[-1, seen, 1:, -1].isnan().all()) and int(got[:, :, 1:].isnan().sum()) == 2 * d * int(seen.sum())
+
+
 def test_a_batch_past_32_bits():
     """200 images of 64 x 64, 16 heads of 80: 3.1e9 elements of q, k and v.  The first and the last image by themselves: dQ has the same bits, dK and dV (whose sums are cut elsewhere) the
     same to a rounding: 1.5 steps of bf16."""
