@@ -72,6 +72,12 @@ int ssam_build_window_table(int g, int ws, int G, int32_t *table);
  * each row).  n_pre: host, optional.  SSAM_EINVAL unless 0 < r <= 1. */
 int ssam_build_block_mask(int S, int mask_block, double r, int32_t *row_ptr, int32_t *col_idx, int *n_pre);
 
+/* The inverse of a gather table on the device: inv[b][idx[b*idx_batch_stride+p]] = p, and -1 for tokens that idx does
+ * not name.  idx dev int32, Nout entries an image (idx_batch_stride = 0 shares one table); those outside [0,N) are slots
+ * without a token; no token twice.  inv dev int32 [B][N], all written.  B*N and B*Nout below 2^31 - 65536, else
+ * SSAM_EUNSUPPORTED. */
+int ssam_invert_rows(const int32_t *idx, int idx_batch_stride, int32_t *inv, int B, int Nout, int N, void *stream);
+
 /* Keep count of the routed MLP (Sec. 4.2): clamp(floor(rho*N + 1e-6), 1, N);
  * negative status on bad arguments. */
 int ssam_keep_count(int N, double rho);
@@ -216,6 +222,81 @@ int ssam_linear_ln(const void *x, int ldx, const float *stats, const void *Wfp, 
                    const float *bias_f, void *C, int ldc, int M, int N, int K,
                    const int32_t *row_map, int rows_per_batch, int map_batch_stride, int dst_rows_per_batch,
                    void *stream);
+
+/* ------------------------------------------------------------------------- */
+/* Contraction in 8-bit integers                                             */
+/* ------------------------------------------------------------------------- */
+
+/* Rows in 8 bits with a scale each: the tokens of an activation, or the output channels of a weight [out, in].
+ * scales[row] = max|x| / 127, codes[row][c] = rint(x * 127 / max|x|), ties to even, in -127..127; the value held is
+ * codes * scale, off by at most max|x| / 254.  Scales below 2^-126 become 2^-126 (off by 2^-127 at most).  Infinity or
+ * NaN in a row makes its scale NaN (codes 0), and with it every product of the row.  x dev bf16 [rows][D]; codes dev
+ * int8 [rows][D]; scales dev fp32 [rows].  D % 16 == 0, D < 131072 (else SSAM_EUNSUPPORTED). */
+int ssam_quantize_rows(const void *x, void *codes, float *scales, long rows, int D, void *stream);
+
+/* ssam_linear on such rows: with v[m][n] = (sum_k A[m][k] W[n][k]) * w_scales[n] * a_scales[m] + bias[n], the sum exact
+ * (32-bit integers), the rest fp32,
+ *   SSAM_EPI_BIAS: C = v   SSAM_EPI_BIAS_GELU: C = gelu_erf(v)   SSAM_EPI_BIAS_SCATTER_ADD: C[dst(m)] += v
+ *   SSAM_EPI_BIAS_SCATTER: C[dst(m)] = v
+ * rounded to bf16 once; dst(m) from the row map as for ssam_linear (entries outside [0, dst_rows_per_batch) skip the
+ * row).  A dev int8, rows of lda bytes; W dev int8 [N], rows of ldw bytes; a_scales dev fp32 [M]; w_scales, bias dev
+ * fp32 [N]; C dev bf16, rows of ldc elements.  lda >= K, ldw >= K, multiples of 16; ldc >= N, a multiple of 8.  Any M;
+ * N % 8 == 0, K % 16 == 0, K < 131072, lda and ldw up to 2^22 and M * N below 2^45 (else SSAM_EUNSUPPORTED).  The result of
+ * a row does not depend on the other rows of the call.  No workspace, no atomics.  Codes are whole numbers: there is no gradient. */
+int ssam_linear_i8(const void *A, int lda, const float *a_scales, const void *W, int ldw, const float *w_scales,
+                   const float *bias, void *C, int ldc, int M, int N, int K, int epilogue, const int32_t *row_map,
+                   int rows_per_batch, int map_batch_stride, int dst_rows_per_batch, void *stream);
+
+/* ------------------------------------------------------------------------- */
+/* From one half of a block into the next                                    */
+/* ------------------------------------------------------------------------- */
+
+/* The branch behind its own LayerNorm and a gate joins the scaled residual stream, whose LayerNorm goes to the rows that
+ * the next half of a block reads.  For token t of image b, with p = src[b*src_batch_stride+t], q = dst[b*dst_batch_stride+t]:
+ *   n = post_g * LN(o[b][p]) + post_b    (post_g, post_b NULL: n = o[b][p])
+ *   x_out[b][t] = bf16(alpha * x[b][t] + gate[b*gate_batch_stride+:] * n)  where 0 <= p < No,  x[b][t] elsewhere
+ *   y[b][q] = pre_g * LN(x_out[b][t]) + pre_b                              where 0 <= q < Ny
+ * Maps are per token: the inverses (ssam_invert_rows) of the tables that ssam_ln_gather, ssam_sparse_attention and
+ * ssam_routed_mlp take.  A batch stride of 0 shares one map (else >= N); src NULL: p = t (No == N); dst NULL: q = t (Ny == N).
+ * dst must not name a row of an image twice.  Rows of y that it does not name are left as they were.
+ *   x dev bf16 [B][N][D]; x_out likewise, all rows written, or x itself: then tokens without a branch are not touched
+ *   o dev bf16 [B][No][D]; NULL: no branch (src, post_g, post_b and gate NULL too; x_out NULL or x)
+ *   gate dev fp32 [D], gate_batch_stride 0, or of every image, gate_batch_stride >= D (a multiple of 4); NULL: 1
+ *   pre_g, pre_b NULL: no second LayerNorm (y and dst NULL too)
+ * LayerNorm with biased variance, two-pass fp32 statistics, eps > 0; sums fp32, each tensor written rounded once; the
+ * second LayerNorm reads the stream as it is stored.
+ * ssam_residual_norm:    y dev bf16 [B][Ny][D], D % 8 == 0.
+ * ssam_residual_norm_i8: the rows of y in 8 bits, as ssam_quantize_rows holds the fp32 ones: codes dev int8 [B][Ny][D],
+ *                        scales dev fp32 [B][Ny]; pre_g and pre_b required; D % 16 == 0 (else SSAM_EUNSUPPORTED).
+ * D <= 2048 and B*N below 2^31 - 65536, else SSAM_EUNSUPPORTED. */
+int ssam_residual_norm(const void *x, void *x_out, const void *o, const int32_t *src, int src_batch_stride,
+                       const float *post_g, const float *post_b, const float *gate, int gate_batch_stride, float alpha,
+                       const float *pre_g, const float *pre_b, const int32_t *dst, int dst_batch_stride, float eps, void *y,
+                       int B, int N, int No, int Ny, int D, void *stream);
+int ssam_residual_norm_i8(const void *x, void *x_out, const void *o, const int32_t *src, int src_batch_stride,
+                          const float *post_g, const float *post_b, const float *gate, int gate_batch_stride, float alpha,
+                          const float *pre_g, const float *pre_b, const int32_t *dst, int dst_batch_stride, float eps,
+                          void *codes, float *scales, int B, int N, int No, int Ny, int D, void *stream);
+
+/* Gradients of ssam_residual_norm.  x_out: the stream that it wrote; o, src, post_g, post_b, gate, alpha, pre_g, dst, eps, sizes
+ * as given to it; dy dev bf16 [B][Ny][D] (NULL with pre_g NULL): the gradient of y; dx_out dev bf16 [B][N][D]: what reaches
+ * x_out from behind (NULL: nothing).  With h the normalised rows (before gain and shift; h = o where there is no first LayerNorm),
+ *   G = dx_out + gradient of the second LayerNorm (dy, where q names a row)
+ *   dx = alpha * G where the token has a branch, G elsewhere
+ *   dn = gate * G;  do[b][p] = gradient of the first LayerNorm (dn);  dgate = sum G * n  (of every image where gate is)
+ *   dpost_g = sum dn * h;  dpost_b = sum dn;  dpre_g = sum dy * h_x;  dpre_b = sum dy
+ * dx dev bf16 [B][N][D], all written, may be dx_out; d_o dev bf16 [B][No][D]: rows that src names are written, others left as
+ * they were; src and dst must not name a row of an image twice.  dgate dev fp32 [D] or [B][D] dense; dpost_g, dpost_b,
+ * dpre_g, dpre_b dev fp32 [D]; any of the five may be NULL: not wanted (each needs what it is the gradient of).  No output may
+ * overlap an input but as said.  Sums are fp32 and in a fixed order: the same inputs give the same bits.  workspace dev,
+ * >= ..._workspace_bytes (gate_images: B where the gate is of every image, else 1), not read where none of the five is wanted. */
+size_t ssam_residual_norm_backward_workspace_bytes(int B, int N, int D, int gate_images);
+int ssam_residual_norm_backward(const void *x_out, const void *o, const int32_t *src, int src_batch_stride,
+                                const float *post_g, const float *post_b, const float *gate, int gate_batch_stride, float alpha,
+                                const float *pre_g, const int32_t *dst, int dst_batch_stride, float eps,
+                                const void *dy, const void *dx_out, void *dx, void *d_o,
+                                float *dgate, float *dpost_g, float *dpost_b, float *dpre_g, float *dpre_b,
+                                int B, int N, int No, int Ny, int D, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- */
 /* Stripe-Sort attention (App. A.1, Alg. 1)                                  */

@@ -55,7 +55,8 @@ def lib():
         for n in ("ssam_score_tokens_workspace_bytes", "ssam_routed_mlp_workspace_bytes",
                   "ssam_encoder_block_workspace_bytes", "ssam_encoder_workspace_bytes", "ssam_linear_workspace_bytes",
                   "ssam_patch_embed_workspace_bytes", "ssam_neck_workspace_bytes",
-                  "ssam_ln_gather_backward_workspace_bytes", "ssam_sparse_attention_backward_workspace_bytes"):
+                  "ssam_ln_gather_backward_workspace_bytes", "ssam_sparse_attention_backward_workspace_bytes",
+                  "ssam_residual_norm_backward_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         L.ssam_probe_mfma_flops.restype = C.c_double
         _lib = L
@@ -694,6 +695,168 @@ def ssam_gelu_backward(codes, scales, da, dh=None, a=None, activation=True):
     _one_device(codes=codes, scales=scales, da=da, dh=dh, a=a)
     _check("ssam_gelu_backward", lib().ssam_gelu_backward(pc, ps, pd, _bf(dh, "dh"), _bf(a, "a"), rows, D, _stream()))
     return dh, a
+
+
+# ------------------------------------------------------------------ 8-bit integers
+def ssam_quantize_rows(x, codes=None, scales=None):
+    """x [..., D] bf16 (tokens, or a weight [out, in]) -> (codes [..., D] int8, scales [...] fp32, one for each row)."""
+    px, D = _bf(x, "x"), x.shape[-1]
+    if codes is None:
+        codes = torch.empty_like(x, dtype=torch.int8)
+    if scales is None:
+        scales = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    _shape(codes, x.shape, "codes")
+    _shape(scales, x.shape[:-1], "scales")
+    _one_device(x=x, codes=codes, scales=scales)
+    _check("ssam_quantize_rows", lib().ssam_quantize_rows(px, _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), C.c_long(x.numel() // D if D else 0), C.c_int(D), _stream()))
+    return codes, scales
+
+
+def ssam_linear_i8(A, a_scales, W, w_scales, bias, C_out=None, epilogue=EPI_BIAS, row_map=None, rows_per_batch=1, map_batch_stride=0, dst_rows_per_batch=1):
+    """A [M,K], W [N,K] int8 with a_scales [M], w_scales [N], bias [N] fp32 -> C [M,N] bf16, or C_out updated through the row map (as for ssam_linear).
+    A, W and C_out may be column slices of wider tensors."""
+    (M, K), N = A.shape, W.shape[0]
+    mapped = epilogue in (EPI_BIAS_SCATTER_ADD, EPI_BIAS_SCATTER)
+    _shape(W, (N, K), "W")
+    for name, t, want in (("a_scales", a_scales, (M,)), ("w_scales", w_scales, (N,)), ("bias", bias, (N,))):
+        _shape(t, want, name)
+    if mapped:
+        if C_out is None or row_map is None or rows_per_batch <= 0:
+            raise ValueError("a mapped epilogue needs C_out, row_map and rows_per_batch")
+        batches = -(-M // rows_per_batch)
+        if row_map.numel() < (batches - 1) * map_batch_stride + M - (batches - 1) * rows_per_batch or (batches > 1 and row_map.numel() < (batches - 2) * map_batch_stride + rows_per_batch):
+            raise ValueError(f"row_map: {row_map.numel()} entries do not cover {M} rows")
+        _shape(C_out, (C_out.shape[0], N), "C")
+        if C_out.shape[0] < batches * dst_rows_per_batch:
+            raise ValueError(f"C: {C_out.shape[0]} rows, expected {batches * dst_rows_per_batch}")
+    elif C_out is None:
+        C_out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)
+    else:
+        _shape(C_out, (M, N), "C")
+    (pa, lda), (pw, ldw), (pc, ldc) = _rows(A, torch.int8, "A"), _rows(W, torch.int8, "W"), _rows(C_out, torch.bfloat16, "C")
+    _one_device(A=A, a_scales=a_scales, W=W, w_scales=w_scales, bias=bias, C=C_out, row_map=row_map)
+    _check("ssam_linear_i8", lib().ssam_linear_i8(
+        pa, lda, _f32(a_scales, "a_scales"), pw, ldw, _f32(w_scales, "w_scales"), _f32(bias, "bias"), pc, ldc, C.c_int(M), C.c_int(N), C.c_int(K),
+        C.c_int(epilogue), _i32(row_map, "row_map"), C.c_int(rows_per_batch), C.c_int(map_batch_stride), C.c_int(dst_rows_per_batch), _stream()))
+    return C_out
+
+
+# ------------------------------------------------------------------ from one half of a block into the next
+def ssam_invert_rows(idx, N, inv=None):
+    """idx int32 [Nout] or [B,Nout]: the token of every slot, outside [0,N) none -> inv int32 [N] or [B,N]: the slot of every token, -1 none."""
+    pi = _i32(idx, "idx")
+    if inv is None:
+        inv = idx.new_empty((*idx.shape[:-1], N))
+    _shape(inv, (*idx.shape[:-1], N), "inv")
+    _one_device(idx=idx, inv=inv)
+    B, Nout = (1, idx.shape[0]) if idx.dim() == 1 else idx.shape
+    _check("ssam_invert_rows", lib().ssam_invert_rows(pi, C.c_int(0 if B == 1 else Nout), _i32(inv, "inv"), C.c_int(B), C.c_int(Nout), C.c_int(N), _stream()))
+    return inv
+
+
+def _token_map(t, B, N, name):
+    """Pointer and batch stride of a map of tokens: [N] or [1,N] for all images, [B,N] for each."""
+    if t is None:
+        return C.c_void_p(0), C.c_int(0)
+    if t.dim() == 2 and t.shape[0] == B and B > 1:
+        _shape(t, (B, N), name)
+        return _i32(t, name), C.c_int(N)
+    _shape(t, (N,) if t.dim() == 1 else (1, N), name)
+    return _i32(t, name), C.c_int(0)
+
+
+def _residual_step(x, o, src, post, gate, dst, pre, eps):
+    """What the calls of a step share: sizes, and their common arguments."""
+    B, N, D = x.shape
+    _bf(x, "x")
+    No = 0 if o is None else o.shape[1]
+    _shape(o, (B, No, D), "o")
+    post_g, post_b = post if post is not None else (None, None)
+    pre_g, pre_b = pre if pre is not None else (None, None)
+    for name, t in (("post gain", post_g), ("post shift", post_b), ("pre gain", pre_g), ("pre shift", pre_b)):
+        _shape(t, (D,), name)
+    stride = 0
+    if gate is not None and gate.dim() == 2:
+        _shape(gate, (B, D), "gate")
+        stride = D
+    else:
+        _shape(gate, (D,), "gate")
+    _one_device(x=x, o=o, src=src, post_g=post_g, post_b=post_b, gate=gate, dst=dst, pre_g=pre_g, pre_b=pre_b)
+    branch = [_bf(o, "o"), *_token_map(src, B, N, "src"), _f32(post_g, "post gain"), _f32(post_b, "post shift"), _f32(gate, "gate"), C.c_int(stride)]
+    return B, N, No, D, branch, (post_g, post_b, pre_g, pre_b), [*_token_map(dst, B, N, "dst"), C.c_float(eps)]
+
+
+def ssam_residual_norm(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre=None, dst=None, eps=1e-6, Ny=None, x_out=None, y=None):
+    """x [B,N,D], o [B,No,D] bf16; src, dst int32 [N] or [B,N] (None: the tokens' own order); post, pre: (gain, shift) fp32 [D] of the LayerNorms behind the branch and
+    in front of the next half, or None; gate fp32 [D] or [B,D] or None -> (x_out [B,N,D], y [B,Ny,D] bf16 or None).
+    x_out may be x; y: rows that dst does not name are left as they are (None: a new one, zeros there)."""
+    B, N, No, D, branch, (post_g, post_b, pre_g, pre_b), tail = _residual_step(x, o, src, post, gate, dst, pre, eps)
+    x_out = (x if o is None else torch.empty_like(x)) if x_out is None else x_out
+    _shape(x_out, x.shape, "x_out")
+    if pre is not None:
+        Ny = y.shape[1] if y is not None else N if Ny is None else Ny
+        if y is None:
+            y = x.new_empty((B, Ny, D)) if dst is None else x.new_zeros((B, Ny, D))
+        _shape(y, (B, Ny, D), "y")
+    _one_device(x_out=x_out, y=y)
+    _check("ssam_residual_norm", lib().ssam_residual_norm(
+        _bf(x, "x"), _bf(x_out, "x_out"), *branch, C.c_float(alpha), _f32(pre_g, "pre gain"), _f32(pre_b, "pre shift"), *tail, _bf(y, "y"),
+        C.c_int(B), C.c_int(N), C.c_int(No), C.c_int(Ny or 0), C.c_int(D), _stream()))
+    return x_out, y
+
+
+def ssam_residual_norm_i8(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre=None, dst=None, eps=1e-6, Ny=None, x_out=None, codes=None, scales=None):
+    """ssam_residual_norm with its rows in 8 bits -> (x_out, codes [B,Ny,D] int8, scales [B,Ny] fp32), the operand of ssam_linear_i8.
+    codes, scales: rows that dst does not name are left as they are (None: new ones, zeros there)."""
+    B, N, No, D, branch, (post_g, post_b, pre_g, pre_b), tail = _residual_step(x, o, src, post, gate, dst, pre, eps)
+    x_out = (x if o is None else torch.empty_like(x)) if x_out is None else x_out
+    _shape(x_out, x.shape, "x_out")
+    Ny = codes.shape[1] if codes is not None else scales.shape[1] if scales is not None else N if Ny is None else Ny
+    new = torch.empty if dst is None else torch.zeros
+    codes = new((B, Ny, D), dtype=torch.int8, device=x.device) if codes is None else codes
+    scales = new((B, Ny), dtype=torch.float32, device=x.device) if scales is None else scales
+    _shape(codes, (B, Ny, D), "codes")
+    _shape(scales, (B, Ny), "scales")
+    _one_device(x_out=x_out, codes=codes, scales=scales)
+    _check("ssam_residual_norm_i8", lib().ssam_residual_norm_i8(
+        _bf(x, "x"), _bf(x_out, "x_out"), *branch, C.c_float(alpha), _f32(pre_g, "pre gain"), _f32(pre_b, "pre shift"), *tail, _dev(codes, torch.int8, "codes"),
+        _f32(scales, "scales"), C.c_int(B), C.c_int(N), C.c_int(No), C.c_int(Ny), C.c_int(D), _stream()))
+    return x_out, codes, scales
+
+
+def ssam_residual_norm_backward_workspace_bytes(B, N, D, gate_images=1) -> int:
+    return lib().ssam_residual_norm_backward_workspace_bytes(C.c_int(B), C.c_int(N), C.c_int(D), C.c_int(gate_images))
+
+
+def ssam_residual_norm_backward(x_out, o=None, src=None, post=None, gate=None, alpha=1.0, pre=None, dst=None, eps=1e-6, dy=None, dx_out=None, dx=None, do=None,
+                                weight_grads=True, workspace=None):
+    """Gradients of ssam_residual_norm: x_out its stream, dy [B,Ny,D] and dx_out [B,N,D] (or None) bf16 the gradients of its results, the rest as given to it
+    -> (dx, do, dgate, (dpost_g, dpost_b) or None, (dpre_g, dpre_b) or None).  dx may be dx_out; do: rows that src does not name are left as they are (None: a new one,
+    zeros there)."""
+    B, N, No, D, branch, (post_g, post_b, pre_g, _), tail = _residual_step(x_out, o, src, post, gate, dst, pre, eps)
+    if pre is None and dy is not None or pre is not None and (dy is None or dy.dim() != 3):
+        raise ValueError("dy: the gradient of y, where there is one")
+    Ny = 0 if dy is None else dy.shape[1]
+    _shape(dy, (B, Ny, D), "dy")
+    dx = torch.empty_like(x_out) if dx is None else dx
+    if do is None and o is not None:
+        do = torch.empty_like(o) if src is None else torch.zeros_like(o)
+    for name, t, want in (("dx_out", dx_out, x_out.shape), ("dx", dx, x_out.shape), ("do", do, (B, No, D))):
+        _shape(t, want, name)
+    dgate = dpost = dpre = None
+    if weight_grads:
+        new = lambda: x_out.new_empty(D, dtype=torch.float32)  # noqa: E731
+        dgate = None if gate is None else torch.empty_like(gate)
+        dpost = None if post is None else (new(), new())
+        dpre = None if pre is None else (new(), new())
+        if workspace is None and (dgate is not None or dpost or dpre):
+            workspace = torch.empty(ssam_residual_norm_backward_workspace_bytes(B, N, D, B if gate is not None and gate.dim() == 2 else 1), dtype=torch.uint8, device=x_out.device)
+    _one_device(dy=dy, dx_out=dx_out, dx=dx, do=do, workspace=workspace)
+    _check("ssam_residual_norm_backward", lib().ssam_residual_norm_backward(
+        _bf(x_out, "x_out"), *branch, C.c_float(alpha), _f32(pre_g, "pre gain"), *tail, _bf(dy, "dy"), _bf(dx_out, "dx_out"), _bf(dx, "dx"), _bf(do, "do"),
+        _f32(dgate, "dgate"), *(_f32(t, "dpost") for t in dpost or (None, None)), *(_f32(t, "dpre") for t in dpre or (None, None)),
+        C.c_int(B), C.c_int(N), C.c_int(No), C.c_int(Ny), C.c_int(D), _dev(workspace, torch.uint8, "workspace"), C.c_size_t(0 if workspace is None else workspace.numel()), _stream()))
+    return dx, do, dgate, dpost, dpre
 
 
 # ------------------------------------------------------------------ instrumentation

@@ -1,7 +1,7 @@
 // What a training step of the block needs beside attention's gradient: the gradient of the LayerNorm of gathered rows, and
 // activations that are kept in 8 bits between the forward and the backward pass, with the GELU that reads them.
 // All of it is bound by HBM: one pass over the data, 16 bytes of bf16 per lane and request.
-#include "common.h"
+#include "rows8.h"
 
 namespace {
 
@@ -196,36 +196,21 @@ struct FastDiv {
     __device__ __forceinline__ uint32_t div(uint32_t n) const { return (__umulhi(n, m) + n) >> shift; }
 };
 
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
-{
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
-
 struct Quantised { uint2 codes; float scale; };
-// v: this lane's eight values of a block (zeros past the row); all eight lanes of the block call it.  Magnitudes of bf16 order as their bits do, infinities and NaN highest.
+// v: this lane's eight values of a block (zeros past the row); all eight lanes of the block call it
 __device__ __forceinline__ Quantised quantise_block(const uint4 &v)
 {
-    constexpr uint32_t MAG = 0x7fff7fffu;
-    uint32_t top = max_u16x2(max_u16x2(v.x & MAG, v.y & MAG), max_u16x2(v.z & MAG, v.w & MAG));
+    uint32_t top = top_of_bf16x8(v);
     top = max(top >> 16, top & 0xffffu);
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
     Quantised r = { make_uint2(0, 0), __uint_as_float(0x7fc00000u) };
     if (top >= 0x7f80u) return r;
-    const float most = bf16_bits_to_float(top);
-    r.scale = fmaxf(most / 127.f, 0x1p-126f);
-    // 127 / most, rounded up.  Half of the largest value is a tie for every block (63.5: 64), and with a factor that is too small by its rounding it came out as 63.  (Other ties need a
-    // largest value of 127 times a power of two, whose factor is exact; and quotients that are no ties are 7e-6 and more from one.)
-    float inv = 127.f / most;
-    if (fmaf(inv, most, -127.f) < 0.f) inv = __uint_as_float(__float_as_uint(inv) + 1u);
-    inv = top ? fminf(inv, 0x1p126f) : 0.f;
+    const RowScale s = row_scale(bf16_bits_to_float(top));
+    r.scale = s.scale;
     float f[8];
     unpack_bf16x8(v, f);
-    int c[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = (int)rintf(f[e] * inv) & 0xff;
-    r.codes = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+    r.codes = codes_of(f, s.inv);
     return r;
 }
 
