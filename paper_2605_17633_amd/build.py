@@ -17,7 +17,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libssam.so")
 SOURCES = ["gemm.hip", "gemm_wide_folded.hip", "gemm_wide_parts.hip", "gemm_large_parts.hip", "gemm_wide_add.hip", "gemm_wide_scatter.hip", "gemm_wide_gelu.hip", "gemm_wide_bias.hip",
-           "attention.hip", "attention_backward.hip", "movers.hip", "tables.hip", "block.hip", "ends.hip", "gradients.hip", "residual.hip", "gemm_i8.hip", "probe.hip"]
+           "attention.hip", "attention_backward.hip", "movers.hip", "tables.hip", "block.hip", "ends.hip", "gradients.hip", "residual.hip", "gemm_i8_bias.hip", "gemm_i8_gelu.hip", "gemm_i8_add.hip",
+           "gemm_i8_scatter.hip", "gemm_i8.hip", "probe.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"),
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function",
          "-Wno-inline-asm"]     # the window attention kernel names m0 in an asm clobber list (LDS-destination loads)
@@ -50,7 +51,7 @@ def _resources(stderr: str):
     return kernels
 
 
-HOT = ("gemm_bf16_nt_", "gemm_ring_kernel", "gemm_direct_kernel", "gemm_wide_kernel", "attn_")     # kernels that are written to a register budget
+HOT = ("gemm_bf16_nt_", "gemm_ring_kernel", "gemm_direct_kernel", "gemm_wide_kernel", "gemm_i8_wide_kernel", "attn_")     # kernels that are written to a register budget
 
 BACKWARD = ("backward_rows_kernel", "backward_columns_kernel", "backward_windows_kernel")                # likewise, of one wave to a SIMD with tables of 128 entries
 

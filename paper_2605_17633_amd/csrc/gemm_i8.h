@@ -1,0 +1,409 @@
+// The contraction of 8-bit integers (gemm_i8.hip) for problems of more than a few rows: gemm_wide.h's schedule on the same bytes.  A slab of K is 128 bytes a row, two k-steps of the
+// 16x16x64 instruction, which reads the registers and takes the time of the bf16 one of 16x16x32: tiles, ring, swizzles and fragments are those of GemmWide.
+// What differs: sums are whole numbers, so that halves of K add up exactly in any order; K is any multiple of 16 (a last slab's requests stay inside the row, and the fragments of one operand are
+// zeros from K on: whatever the other one holds there adds nothing); the epilogue scales by row and column.
+#pragma once
+
+#include "gemm_wide.h"
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+struct GemmI8Args {
+    const unsigned char *A, *W;
+    const float *a_scales, *w_scales, *bias;
+    bf16 *C;
+    int M, N, K;
+    GemmLd ld;
+    GemmRowMap rm;
+};
+
+constexpr int GEMM_I8_BK = 2 * GEMM_BK;       // bytes of K in a slab
+
+// Sum, scales and bias of a value of C.
+template <int EPI>
+__device__ __forceinline__ float gemm_i8_value(int acc, float w_scale, float a_scale, float bias)
+{
+    const float v = fmaf((float)acc * w_scale, a_scale, bias);
+    return EPI == SSAM_EPI_BIAS_GELU ? gelu_erf(v) : v;
+}
+
+// Destination row of row m of the product, -1: none.
+template <int EPI>
+__device__ __forceinline__ int gemm_i8_row(const GemmI8Args &a, int m)
+{
+    if (m >= a.M) return -1;
+    if constexpr (EPI != SSAM_EPI_BIAS_SCATTER_ADD && EPI != SSAM_EPI_BIAS_SCATTER) return m;
+    const int b = m / a.rm.rows_per_batch;
+    const int idx = a.rm.map[(long)b * a.rm.map_batch_stride + (m - b * a.rm.rows_per_batch)];
+    return (unsigned)idx < (unsigned)a.rm.dst_rows_per_batch ? b * a.rm.dst_rows_per_batch + idx : -1;
+}
+
+template <int BM, int BN, int WGK, int EPI>
+__global__ void __launch_bounds__(512, 1)
+gemm_i8_wide_kernel(GemmI8Args a, GemmTileRange tr)
+{
+    using G = GemmWide<BM, BN, WGK>;
+    constexpr int WGN = G::WGN, MT = G::MT, NT = G::NT, NP = NT / 2, WM = MT * 16, WN = NT * 16, SA = G::SA, SW = G::SW, L = G::L;
+    constexpr bool ADD = EPI == SSAM_EPI_BIAS_SCATTER_ADD, EARLY = MT * NT < 24;       // registers for what the epilogue reads before the last slabs
+    static_assert(!EARLY || G::EARLY, "and LDS for the row map");
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    // WGK == 1: SA slabs of A, then SW of W; 2: slab by slab, A then W
+    constexpr int STRIDE_A = WGK == 1 ? G::AB : G::AB + G::WB, STRIDE_W = WGK == 1 ? G::WB : G::AB + G::WB, W0 = WGK == 1 ? SA * G::AB : G::AB;
+    unsigned char *as = smem, *ws = smem + W0;
+    using std::integral_constant;
+
+    const int per_xcd = (tr.tile_count + 7) / 8, tl = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (tl >= tr.tile_count) return;
+    int m0, n0;
+    gemm_tile_origin(tr, tl, 0, 1, 1, BM, BN, m0, n0);
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wk = wave * WGK >> 3, wt = wave & (8 / WGK - 1), wm = wt / WGN * WM, wn = wt % WGN * WN;
+    const int l16 = lane & 15, quad = lane >> 4;
+    const int n = (a.K + GEMM_I8_BK - 1) / GEMM_I8_BK, last = (a.K - (n - 1) * GEMM_I8_BK) / 16;      // slabs, and 16-byte chunks of the last one
+
+    // column of C (from the wave's first) of operand row l of its MFMA tile j: a lane then holds 8 consecutive columns of a pair of tiles
+    auto perm = [](int j, int l) { return j < 2 * NP ? 32 * (j >> 1) + (l >> 2) * 8 + (j & 1) * 4 + (l & 3) : 16 * j + l; };
+
+    // ---- requests: 1 KB each, A's of a slab, then W's; wave w takes w, w + 8, ...  Rows past the end repeat the last one; nothing of them is stored.
+    static_assert(G::QA % 2 == 0, "a wave's requests all have the same swizzle");
+    const int chunk = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);                    // of a row's slab, that this lane asks for
+    const uint32_t back = (uint32_t)(chunk - min(chunk, last - 1)) * 16;                    // by so much further in front in the last slab
+    uint32_t off[L], dst[L];
+    const unsigned char *base[L];
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char *)smem);
+    auto is_a = [&](int i) { return WGK == 1 ? i < G::QA / 8 : i * 8 + wave < G::QA; };
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const int f = i * 8 + wave;
+        if (is_a(i)) {
+            off[i] = (uint32_t)(min(m0 + f * 8 + (lane >> 3), a.M - 1) - m0) * (uint32_t)a.ld.a + chunk * 16;
+            base[i] = a.A + (long)m0 * a.ld.a;
+            dst[i] = lds0 + f * 1024;
+        } else {
+            const int w = f - G::QA, row = w * 8 + (lane >> 3), h = row / WN, q = row % WN;
+            off[i] = (uint32_t)(min(n0 + h * WN + perm(q >> 4, q & 15), a.N - 1) - n0) * (uint32_t)a.ld.w + chunk * 16;
+            base[i] = a.W + (long)n0 * a.ld.w;
+            dst[i] = lds0 + W0 + w * 1024;
+        }
+    }
+    const bool all = G::LREST == 0 || wave < G::LREST;              // this wave has an L-th request
+    auto request = [&](int i, int sa, int sw) {
+        if (G::LREST != 0 && i == L - 1 && !all) return;
+        gemm_load_lds16_s(dst[i] + (WGK == 1 && i >= G::QA / 8 ? sw * STRIDE_W : sa * STRIDE_A), off[i], base[i]);
+        base[i] += GEMM_I8_BK;
+    };
+    // in front of the requests [from, to) of slab t
+    auto ahead = [&](int t, int from, int to) {
+        if (t != n - 1) return;
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+            if (i >= from && i < to) off[i] -= back;
+    };
+    // waits until the slab before the last `rem` requested ones has landed; MAX: the most that rem can be
+    auto wait_slabs = [&](int rem, auto max_) {
+        constexpr int MAX = decltype(max_)::value;
+        auto out = [&](auto slabs) {                // no more than the requests of `slabs` slabs still out (of W's at most MAX - (SA - SW))
+            constexpr int s = decltype(slabs)::value, w = s < MAX - (SA - SW) ? s : MAX - (SA - SW);
+            if constexpr (WGK == 1) gemm_wait_vm<G::QA / 8 * s + G::QW / 8 * w>();
+            else if (G::LREST != 0 && !all) gemm_wait_vm<(L - 1) * s>();
+            else gemm_wait_vm<L * s>();
+        };
+        if (rem >= MAX) out(integral_constant<int, MAX>{});
+        else if (MAX > 2 && rem >= 2) out(integral_constant<int, 2>{});
+        else if (MAX > 1 && rem >= 1) out(integral_constant<int, 1>{});
+        else gemm_wait_vm<0>();
+    };
+    constexpr int LA = G::QA / 8, LW = G::QW / 8;   // WGK == 1: requests per wave of A and of W
+
+    // ---- fragments: operand a = 16 columns of C (rows of W), operand b = 16 rows
+    const uint32_t fa0 = (wm + l16) * 128 + ((quad ^ ((l16 >> 1) & 7)) << 4), fw0 = (wn + l16) * 128 + ((quad ^ ((l16 >> 1) & 7)) << 4);
+    i32x4 fa[2][MT], fw[2][NT], acc[MT][NT] = {};
+    // read q of k-step s of a slab into set b, in the order its MFMAs want them
+    auto read = [&](int q, int b, int s, int sa, int sw) {
+        if (q == 0 || q > NT) {
+            const int i = q == 0 ? 0 : q - NT;
+            fa[b][i] = *reinterpret_cast<const i32x4 *>(as + sa * STRIDE_A + (fa0 ^ (s * 64)) + i * 2048);
+        } else {
+            fw[b][q - 1] = *reinterpret_cast<const i32x4 *>(ws + sw * STRIDE_W + (fw0 ^ (s * 64)) + (q - 1) * 2048);
+        }
+    };
+    // of the last slab: what lies past K is zeros in one operand
+    auto cut = [&](int b, int s) {
+        if (last == 8) return;
+        const bool past = 4 * s + quad >= last;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) fw[b][j][e] = past ? 0 : fw[b][j][e];
+    };
+    constexpr int NM = MT * NT, NR = MT + NT;
+    auto mfma = [&](int m, int b) {
+        const int i = m / NT, j = m % NT;
+        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[b][j], fa[b][i], acc[i][j], 0, 0, 0);
+    };
+
+    // ---- what the epilogue reads (group wk of two finishes rows i of its MTH, from wk * MTH on): requested before the last slabs, the row map in front of the first one,
+    // since a wait for an ordinary load also waits for every request in front of it
+    constexpr int MTH = (MT + WGK - 1) / WGK, NB = NP * 2 + NT % 2;          // NB: groups of 4 columns
+    constexpr bool MAPPED = ADD || EPI == SSAM_EPI_BIAS_SCATTER;
+    const int ncol = n0 + wn + quad * 8, ncol1 = n0 + wn + 32 * NP + quad * 4;      // first column of pair 0, of the odd tile
+    if constexpr (MAPPED && EARLY) {
+        if (wave * 64 < BM) {
+            const int m = min(m0 + wave * 64 + lane, a.M - 1), b = m / a.rm.rows_per_batch;
+            gemm_load_lds4(lds0 + (uint32_t)G::ring + wave * 256, a.rm.map + (long)b * a.rm.map_batch_stride + (m - b * a.rm.rows_per_batch));
+        }
+    }
+    int drow[MTH];                                // destination rows, -1: not stored
+    float rs[MTH];
+    f32x4 bv[NB], cs[NB];
+    constexpr int ROW = NP * 4 + NT % 2 * 2, AHEAD = !ADD ? 1 : ROW * MTH <= 32 ? MTH : 32 / ROW;      // rows whose old values are requested ahead
+    uint4 old[ADD ? AHEAD : 1][NP > 0 ? NP : 1];
+    uint2 old1[ADD ? AHEAD : 1];
+    auto load_old = [&](int k) {
+        const bf16 *row = a.C + (long)max(drow[k], 0) * a.ld.c;      // a row that is not stored reads row 0 and drops the value
+#pragma unroll
+        for (int p = 0; p < NP; ++p) old[k % AHEAD][p] = *reinterpret_cast<const uint4 *>(row + (ncol + 32 * p < a.N ? ncol + 32 * p : 0));
+        if constexpr (NT % 2) old1[k % AHEAD] = *reinterpret_cast<const uint2 *>(row + (ncol1 < a.N ? ncol1 : 0));
+    };
+    auto load_epilogue = [&]() {
+#pragma unroll
+        for (int k = 0; k < MTH; ++k) {
+            const int i = wk * MTH + k, row = wm + 16 * i + l16, m = m0 + row;
+            if constexpr (MAPPED && EARLY) {
+                const int b = min(m, a.M - 1) / a.rm.rows_per_batch, idx = reinterpret_cast<const int32_t *>(smem + G::ring)[row < BM ? row : 0];
+                drow[k] = m < a.M && (unsigned)idx < (unsigned)a.rm.dst_rows_per_batch ? b * a.rm.dst_rows_per_batch + idx : -1;
+            } else {
+                drow[k] = gemm_i8_row<EPI>(a, m);
+            }
+            if (MTH * WGK != MT && i >= MT) drow[k] = -1;
+            rs[k] = a.a_scales[min(m, a.M - 1)];
+        }
+        if constexpr (ADD) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) load_old(k);
+        }
+#pragma unroll
+        for (int g = 0; g < NB; ++g) {
+            int c = g < 2 * NP ? ncol + 32 * (g >> 1) + 4 * (g & 1) : ncol1;
+            c = c < a.N ? c : 0;
+            bv[g] = *reinterpret_cast<const f32x4 *>(a.bias + c);
+            cs[g] = *reinterpret_cast<const f32x4 *>(a.w_scales + c);
+        }
+    };
+
+    // ---- ring
+    int sa = 0, sw = 0;                          // stages of slab t
+    if constexpr (WGK == 1) {
+        // iteration t of the loop requests W of slab t + SW, then A of slab t + SA; here those of t = -SA .. -1
+#pragma unroll
+        for (int t = -SA; t < 0; ++t) {
+            if (t + SW >= 0 && t + SW < n) {
+                ahead(t + SW, LA, L);
+#pragma unroll
+                for (int i = LA; i < L; ++i) request(i, 0, t + SW);
+            }
+            if (t + SA < n) {
+                ahead(t + SA, 0, LA);
+#pragma unroll
+                for (int i = 0; i < LA; ++i) request(i, t + SA, 0);
+            }
+        }
+        wait_slabs(n - 1, integral_constant<int, SA - 1>{});
+        LDS_BARRIER();
+#pragma unroll
+        for (int q = 0; q < NR; ++q) read(q, 0, 0, 0, 0);
+        auto slab = [&](int t, auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            const int sa1 = sa + 1 == SA ? 0 : sa + 1, sw1 = sw + 1 == SW ? 0 : sw + 1;
+            if constexpr (FULL) {
+                ahead(t + SW, LA, L);
+                ahead(t + SA, 0, LA);
+            } else if (t == n - 1) {
+                cut(0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int m = 0; m < NM; ++m) {
+                mfma(m, 0);
+#pragma unroll
+                for (int q = m * NR / NM; q < (m + 1) * NR / NM; ++q) read(q, 1, 1, sa, sw);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // slab t + 1 has landed when no more than the requests behind it are out; every wave has read all of slab t
+            wait_slabs(FULL ? SA : n - 2 - t, integral_constant<int, SA - 2>{});
+            LDS_BARRIER();
+            if constexpr (FULL) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int m = 0; m < NM; ++m) {
+                    mfma(m, 1);
+#pragma unroll
+                    for (int q = m * NR / NM; q < (m + 1) * NR / NM; ++q) read(q, 0, 0, sa1, sw1);
+#pragma unroll
+                    for (int q = m * L / NM; q < (m + 1) * L / NM; ++q) request(q < LW ? LA + q : q - LW, sa, sw);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                if (t + SW < n) {
+                    ahead(t + SW, LA, L);
+#pragma unroll
+                    for (int i = LA; i < L; ++i) request(i, sa, sw);
+                }
+                if (t == n - 1) cut(1, 1);
+                if (t + 1 < n)
+#pragma unroll
+                    for (int q = 0; q < NR; ++q) read(q, 0, 0, sa1, sw1);
+#pragma unroll
+                for (int m = 0; m < NM; ++m) mfma(m, 1);
+            }
+            sa = sa1;
+            sw = sw1;
+        };
+        int t = 0;
+        for (; t < n - SA; ++t) slab(t, std::true_type{});
+        if (EARLY) load_epilogue();
+#pragma unroll 1
+        for (; t < n; ++t) slab(t, std::false_type{});
+    } else {
+        constexpr int S = SA;
+#pragma unroll
+        for (int t = 0; t < S; ++t)
+            if (t < n) {
+                ahead(t, 0, L);
+#pragma unroll
+                for (int i = 0; i < L; ++i) request(i, t, t);
+            }
+        wait_slabs(n - 1, integral_constant<int, S - 1>{});
+        LDS_BARRIER();
+#pragma unroll
+        for (int q = 0; q < NR; ++q) read(q, 0, wk, 0, 0);
+        // slab t from set B; its stage, which every wave has read, takes slab t + S
+        auto slab = [&](int t, auto set, auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            constexpr int B = decltype(set)::value;
+            const int s1 = sa + 1 == S ? 0 : sa + 1;
+            if constexpr (FULL) ahead(t + S, 0, L);
+            else if (t == n - 1) cut(B, wk);
+            wait_slabs(FULL ? S : n - 2 - t, integral_constant<int, S - 2>{});
+            LDS_BARRIER();
+            if constexpr (FULL) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int m = 0; m < NM; ++m) {
+                    mfma(m, B);
+#pragma unroll
+                    for (int q = m * NR / NM; q < (m + 1) * NR / NM; ++q) read(q, B ^ 1, wk, s1, s1);
+#pragma unroll
+                    for (int q = m * L / NM; q < (m + 1) * L / NM; ++q) request(q, sa, sa);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                if (t + 1 < n)
+#pragma unroll
+                    for (int q = 0; q < NR; ++q) read(q, B ^ 1, wk, s1, s1);
+#pragma unroll
+                for (int m = 0; m < NM; ++m) mfma(m, B);
+            }
+            sa = s1;
+        };
+        int t = 0;
+        for (; t < n - S; t += 2) {
+            slab(t, integral_constant<int, 0>{}, std::true_type{});
+            if (t + 1 >= n - S) break;
+            slab(t + 1, integral_constant<int, 1>{}, std::true_type{});
+        }
+        t = n > S ? n - S : 0;
+        if (EARLY) load_epilogue();
+#pragma unroll 1
+        for (; t < n; ++t) {
+            if (t & 1) slab(t, integral_constant<int, 1>{}, std::false_type{});
+            else slab(t, integral_constant<int, 0>{}, std::false_type{});
+        }
+    }
+    if (!EARLY) load_epilogue();
+
+    // ---- epilogue, straight from the accumulators: lane (l16, quad) holds row 16*i + l16, columns 8*quad .. + 7 of every pair of tiles
+    i32x4 fin[MTH][NT];
+    if constexpr (WGK == 2) {
+        // the halves of K: either group sends the rows that the other one finishes, through the ring, whose last slab every wave had read at the last barrier
+        i32x4 *x = reinterpret_cast<i32x4 *>(smem) + wt * (2 * MTH * NT * 64) + lane;
+#pragma unroll
+        for (int k = 0; k < MTH; ++k)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int hi = MTH + k < MT ? MTH + k : MT - 1;
+                x[((wk ^ 1) * MTH + k) * NT * 64 + j * 64] = wk ? acc[k][j] : acc[hi][j];
+                fin[k][j] = wk ? acc[hi][j] : acc[k][j];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < MTH; ++k)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fin[k][j] += x[(wk * MTH + k) * NT * 64 + j * 64];
+    } else {
+#pragma unroll
+        for (int k = 0; k < MTH; ++k)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fin[k][j] = acc[k][j];
+    }
+#pragma unroll
+    for (int k = 0; k < MTH; ++k) {
+        bf16 *row = a.C + (long)drow[k] * a.ld.c;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gemm_i8_value<EPI>(fin[k][2 * p + e / 4][e % 4], cs[2 * p + e / 4][e % 4], rs[k], bv[2 * p + e / 4][e % 4]);
+            if constexpr (ADD) {
+                float o[8];
+                unpack_bf16x8(old[k % AHEAD][p], o);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += o[e];
+            }
+            if (drow[k] >= 0 && ncol + 32 * p < a.N) *reinterpret_cast<uint4 *>(row + ncol + 32 * p) = pack_bf16x8(v);      // N % 8 == 0
+        }
+        if constexpr (NT % 2) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = gemm_i8_value<EPI>(fin[k][NT - 1][e], cs[2 * NP][e], rs[k], bv[2 * NP][e]);
+            if constexpr (ADD) {
+                v[0] += __uint_as_float(old1[k % AHEAD].x << 16); v[1] += __uint_as_float(old1[k % AHEAD].x & 0xffff0000u);
+                v[2] += __uint_as_float(old1[k % AHEAD].y << 16); v[3] += __uint_as_float(old1[k % AHEAD].y & 0xffff0000u);
+            }
+            if (drow[k] >= 0 && ncol1 < a.N) *reinterpret_cast<uint2 *>(row + ncol1) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        }
+        if constexpr (ADD) if (k + AHEAD < MTH) load_old(k + AHEAD);
+    }
+}
+
+template <int BM, int BN, int WGK, int EPI>
+int gemm_i8_launch_tile(const GemmI8Args &a, hipStream_t st)
+{
+    constexpr size_t lds = GemmWide<BM, BN, WGK>::lds_bytes;
+    auto kern = gemm_i8_wide_kernel<BM, BN, WGK, EPI>;
+    // more than 64 KiB of LDS per workgroup needs the per-kernel opt-in (idempotent, host-side only)
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return SSAM_EHIP;
+    GemmTileRange tr = { ssam_div_up(a.M, BM), ssam_div_up(a.N, BN), 0, 0 };
+    tr.tile_count = tr.tiles_m * tr.tiles_n;
+    hipLaunchKernelGGL(kern, dim3(ssam_div_up(tr.tile_count, 8) * 8), dim3(512), lds, st, a, tr);
+    SSAM_CHECK_LAUNCH();
+    return SSAM_OK;
+}
+
+// Tiles, in the order of their index in the time model (gemm_i8.hip).
+#define GEMM_I8_TILES(X)                                                                                       \
+    X(0, 64, 64, 2) X(1, 96, 64, 2) X(2, 96, 96, 2) X(3, 64, 128, 2) X(4, 128, 128, 1) X(5, 128, 192, 1)         \
+    X(6, 192, 128, 1) X(7, 256, 128, 1) X(8, 192, 192, 1) X(9, 192, 256, 1) X(10, 256, 192, 1) X(11, 256, 256, 1)
+constexpr int GEMM_I8_COUNT = 12;
+
+template <int EPI>
+int gemm_i8_launch(int tile, const GemmI8Args &a, hipStream_t st)
+{
+    switch (tile) {
+#define X(id, bm, bn, wgk) case id: return gemm_i8_launch_tile<bm, bn, wgk, EPI>(a, st);
+    GEMM_I8_TILES(X)
+#undef X
+    default: return SSAM_EINVAL;
+    }
+}

@@ -1,0 +1,4 @@
+// The 8-bit contraction's tiles, epilogue SSAM_EPI_BIAS.
+#include "gemm_i8.h"
+
+int ssam_gemm_i8_bias(int tile, const GemmI8Args &a, hipStream_t st) { return gemm_i8_launch<SSAM_EPI_BIAS>(tile, a, st); }
