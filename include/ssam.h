@@ -290,7 +290,8 @@ int ssam_residual_norm_i8(const void *x, void *x_out, const void *o, const int32
  * they were; src and dst must not name a row of an image twice.  dgate dev fp32 [D] or [B][D] dense; dpost_g, dpost_b,
  * dpre_g, dpre_b dev fp32 [D]; any of the five may be NULL: not wanted (each needs what it is the gradient of).  No output may
  * overlap an input but as said.  Sums are fp32 and in a fixed order: the same inputs give the same bits.  workspace dev,
- * >= ..._workspace_bytes (gate_images: B where the gate is of every image, else 1), not read where none of the five is wanted. */
+ * >= ..._workspace_bytes (gate_images: B where the gate is of every image, else 1), not read where none of the five is wanted.
+ * Limits as for the forward call; at most 65535 images with a gate of every image. */
 size_t ssam_residual_norm_backward_workspace_bytes(int B, int N, int D, int gate_images);
 int ssam_residual_norm_backward(const void *x_out, const void *o, const int32_t *src, int src_batch_stride,
                                 const float *post_g, const float *post_b, const float *gate, int gate_batch_stride, float alpha,

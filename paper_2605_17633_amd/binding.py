@@ -44,6 +44,14 @@ class BlockCfg(C.Structure):
                 ("content_order", C.c_int), ("stripe", C.c_int)]
 
 
+# Argument types of the calls that take plain numbers and addresses (p: pointer, i: int, l: long, f: float, z: size_t): building the ctypes objects in Python took
+# 1 to 3 us of a call of 10 to 20.
+_KINDS = {"p": C.c_void_p, "i": C.c_int, "l": C.c_long, "f": C.c_float, "z": C.c_size_t}
+_ARGUMENTS = {"ssam_quantize_rows": "ppplip", "ssam_linear_i8": "pippippp" + "iiiii" + "piiip", "ssam_invert_rows": "pipiiip",
+              "ssam_residual_norm": "ppppipppifpppifp" + "iiiiip", "ssam_residual_norm_i8": "ppppipppifpppifpp" + "iiiiip",
+              "ssam_residual_norm_backward": "pppipppifppif" + "pppp" + "ppppp" + "iiiiipzp"}
+
+
 def lib():
     """Load libssam.so; fail loudly if it is missing (there is no fallback path)."""
     global _lib
@@ -59,6 +67,8 @@ def lib():
                   "ssam_residual_norm_backward_workspace_bytes"):
             getattr(L, n).restype = C.c_size_t
         L.ssam_probe_mfma_flops.restype = C.c_double
+        for n, kinds in _ARGUMENTS.items():
+            getattr(L, n).argtypes = [_KINDS[k] for k in kinds]
         _lib = L
     return _lib
 
@@ -698,17 +708,49 @@ def ssam_gelu_backward(codes, scales, da, dh=None, a=None, activation=True):
 
 
 # ------------------------------------------------------------------ 8-bit integers
+_BF16, _FP32, _INT32, _INT8, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
+
+
+def _address(t, dtype, here, name):
+    """Address of a dense tensor on the current device, None for None (what _dev and _one_device check, in fewer steps)."""
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous() and t.get_device() == here:
+        return t.data_ptr()
+    _dev(t, dtype, name)
+    _one_device(**{name: t})
+    raise TypeError(f"{name}: expected a contiguous device tensor of {dtype}")
+
+
+def _here(t, name):
+    """The current device, for a call whose first tensor is t (without a GPU there is none to ask for)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError(f"{name}: expected a device tensor")
+    return _device()
+
+
+def _address_rows(t, dtype, here, name):
+    """Address and row stride of a 2-D tensor whose rows are contiguous (a column slice is fine)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 2 and t.get_device() == here:
+        stride, step = t.stride()
+        if step == 1:
+            return t.data_ptr(), stride
+    _rows(t, dtype, name)
+    _one_device(**{name: t})
+    raise TypeError(f"{name}: expected a 2-D device tensor of {dtype} with contiguous rows")
+
+
 def ssam_quantize_rows(x, codes=None, scales=None):
     """x [..., D] bf16 (tokens, or a weight [out, in]) -> (codes [..., D] int8, scales [...] fp32, one for each row)."""
-    px, D = _bf(x, "x"), x.shape[-1]
+    here, shape = _here(x, "x"), x.shape
+    px, D = _address(x, _BF16, here, "x"), shape[-1]
     if codes is None:
-        codes = torch.empty_like(x, dtype=torch.int8)
+        codes = torch.empty_like(x, dtype=_INT8)
     if scales is None:
-        scales = x.new_empty(x.shape[:-1], dtype=torch.float32)
-    _shape(codes, x.shape, "codes")
-    _shape(scales, x.shape[:-1], "scales")
-    _one_device(x=x, codes=codes, scales=scales)
-    _check("ssam_quantize_rows", lib().ssam_quantize_rows(px, _dev(codes, torch.int8, "codes"), _f32(scales, "scales"), C.c_long(x.numel() // D if D else 0), C.c_int(D), _stream()))
+        scales = x.new_empty(shape[:-1], dtype=_FP32)
+    _shape(codes, shape, "codes")
+    _shape(scales, shape[:-1], "scales")
+    _check("ssam_quantize_rows", lib().ssam_quantize_rows(px, _address(codes, _INT8, here, "codes"), _address(scales, _FP32, here, "scales"), x.numel() // D if D else 0, D, _stream()))
     return codes, scales
 
 
@@ -718,114 +760,115 @@ def ssam_linear_i8(A, a_scales, W, w_scales, bias, C_out=None, epilogue=EPI_BIAS
     (M, K), N = A.shape, W.shape[0]
     mapped = epilogue in (EPI_BIAS_SCATTER_ADD, EPI_BIAS_SCATTER)
     _shape(W, (N, K), "W")
-    for name, t, want in (("a_scales", a_scales, (M,)), ("w_scales", w_scales, (N,)), ("bias", bias, (N,))):
-        _shape(t, want, name)
+    _shape(a_scales, (M,), "a_scales")
+    _shape(w_scales, (N,), "w_scales")
+    _shape(bias, (N,), "bias")
     if mapped:
         if C_out is None or row_map is None or rows_per_batch <= 0:
             raise ValueError("a mapped epilogue needs C_out, row_map and rows_per_batch")
         batches = -(-M // rows_per_batch)
-        if row_map.numel() < (batches - 1) * map_batch_stride + M - (batches - 1) * rows_per_batch or (batches > 1 and row_map.numel() < (batches - 2) * map_batch_stride + rows_per_batch):
+        if row_map.numel() < max((batches - 1) * map_batch_stride + M - (batches - 1) * rows_per_batch, (batches - 2) * map_batch_stride + rows_per_batch if batches > 1 else 0):
             raise ValueError(f"row_map: {row_map.numel()} entries do not cover {M} rows")
-        _shape(C_out, (C_out.shape[0], N), "C")
-        if C_out.shape[0] < batches * dst_rows_per_batch:
-            raise ValueError(f"C: {C_out.shape[0]} rows, expected {batches * dst_rows_per_batch}")
+        if C_out.dim() != 2 or C_out.shape[1] != N or C_out.shape[0] < batches * dst_rows_per_batch:
+            raise ValueError(f"C: shape {tuple(C_out.shape)}, expected [{batches * dst_rows_per_batch}, {N}] or more rows")
     elif C_out is None:
-        C_out = torch.empty((M, N), dtype=torch.bfloat16, device=A.device)
+        C_out = A.new_empty((M, N), dtype=_BF16)
     else:
         _shape(C_out, (M, N), "C")
-    (pa, lda), (pw, ldw), (pc, ldc) = _rows(A, torch.int8, "A"), _rows(W, torch.int8, "W"), _rows(C_out, torch.bfloat16, "C")
-    _one_device(A=A, a_scales=a_scales, W=W, w_scales=w_scales, bias=bias, C=C_out, row_map=row_map)
+    here = _here(A, "A")
+    (pa, lda), (pw, ldw), (pc, ldc) = _address_rows(A, _INT8, here, "A"), _address_rows(W, _INT8, here, "W"), _address_rows(C_out, _BF16, here, "C")
     _check("ssam_linear_i8", lib().ssam_linear_i8(
-        pa, lda, _f32(a_scales, "a_scales"), pw, ldw, _f32(w_scales, "w_scales"), _f32(bias, "bias"), pc, ldc, C.c_int(M), C.c_int(N), C.c_int(K),
-        C.c_int(epilogue), _i32(row_map, "row_map"), C.c_int(rows_per_batch), C.c_int(map_batch_stride), C.c_int(dst_rows_per_batch), _stream()))
+        pa, lda, _address(a_scales, _FP32, here, "a_scales"), pw, ldw, _address(w_scales, _FP32, here, "w_scales"), _address(bias, _FP32, here, "bias"), pc, ldc, M, N, K,
+        epilogue, _address(row_map, _INT32, here, "row_map"), rows_per_batch, map_batch_stride, dst_rows_per_batch, _stream()))
     return C_out
 
 
 # ------------------------------------------------------------------ from one half of a block into the next
 def ssam_invert_rows(idx, N, inv=None):
     """idx int32 [Nout] or [B,Nout]: the token of every slot, outside [0,N) none -> inv int32 [N] or [B,N]: the slot of every token, -1 none."""
-    pi = _i32(idx, "idx")
+    here = _here(idx, "idx")
+    pi = _address(idx, _INT32, here, "idx")
     if inv is None:
         inv = idx.new_empty((*idx.shape[:-1], N))
     _shape(inv, (*idx.shape[:-1], N), "inv")
-    _one_device(idx=idx, inv=inv)
     B, Nout = (1, idx.shape[0]) if idx.dim() == 1 else idx.shape
-    _check("ssam_invert_rows", lib().ssam_invert_rows(pi, C.c_int(0 if B == 1 else Nout), _i32(inv, "inv"), C.c_int(B), C.c_int(Nout), C.c_int(N), _stream()))
+    _check("ssam_invert_rows", lib().ssam_invert_rows(pi, 0 if B == 1 else Nout, _address(inv, _INT32, here, "inv"), B, Nout, N, _stream()))
     return inv
 
 
-def _token_map(t, B, N, name):
-    """Pointer and batch stride of a map of tokens: [N] or [1,N] for all images, [B,N] for each."""
+def _token_map(t, B, N, here, name):
+    """Address and batch stride of a map of tokens: [N] or [1,N] for all images, [B,N] for each."""
     if t is None:
-        return C.c_void_p(0), C.c_int(0)
-    if t.dim() == 2 and t.shape[0] == B and B > 1:
-        _shape(t, (B, N), name)
-        return _i32(t, name), C.c_int(N)
-    _shape(t, (N,) if t.dim() == 1 else (1, N), name)
-    return _i32(t, name), C.c_int(0)
+        return None, 0
+    each = t.dim() == 2 and B > 1 and t.shape[0] == B
+    _shape(t, (B, N) if each else (N,) if t.dim() == 1 else (1, N), name)
+    return _address(t, _INT32, here, name), N if each else 0
 
 
-def _residual_step(x, o, src, post, gate, dst, pre, eps):
-    """What the calls of a step share: sizes, and their common arguments."""
-    B, N, D = x.shape
-    _bf(x, "x")
+def _norm(pair, D, here, name):
+    if pair is None:
+        return None, None
+    gain, shift = pair
+    _shape(gain, (D,), name)
+    _shape(shift, (D,), name)
+    return _address(gain, _FP32, here, name), _address(shift, _FP32, here, name)
+
+
+def _step_arguments(x, o, src, post, gate, dst, pre):
+    """What the calls of a step share -> device, sizes, (o, src, its stride, post gain and shift, gate, its stride), (pre gain, shift), (dst, its stride)"""
+    here, (B, N, D) = _here(x, "x"), x.shape
     No = 0 if o is None else o.shape[1]
     _shape(o, (B, No, D), "o")
-    post_g, post_b = post if post is not None else (None, None)
-    pre_g, pre_b = pre if pre is not None else (None, None)
-    for name, t in (("post gain", post_g), ("post shift", post_b), ("pre gain", pre_g), ("pre shift", pre_b)):
-        _shape(t, (D,), name)
-    stride = 0
-    if gate is not None and gate.dim() == 2:
-        _shape(gate, (B, D), "gate")
-        stride = D
-    else:
-        _shape(gate, (D,), "gate")
-    _one_device(x=x, o=o, src=src, post_g=post_g, post_b=post_b, gate=gate, dst=dst, pre_g=pre_g, pre_b=pre_b)
-    branch = [_bf(o, "o"), *_token_map(src, B, N, "src"), _f32(post_g, "post gain"), _f32(post_b, "post shift"), _f32(gate, "gate"), C.c_int(stride)]
-    return B, N, No, D, branch, (post_g, post_b, pre_g, pre_b), [*_token_map(dst, B, N, "dst"), C.c_float(eps)]
+    each = gate is not None and gate.dim() == 2
+    _shape(gate, (B, D) if each else (D,), "gate")
+    branch = (_address(o, _BF16, here, "o"), *_token_map(src, B, N, here, "src"), *_norm(post, D, here, "post"), _address(gate, _FP32, here, "gate"), D if each else 0)
+    return here, B, N, No, D, branch, _norm(pre, D, here, "pre"), _token_map(dst, B, N, here, "dst")
+
+
+def _stream_out(x, o, x_out):
+    if x_out is None:
+        return x if o is None else torch.empty_like(x)
+    _shape(x_out, x.shape, "x_out")
+    return x_out
 
 
 def ssam_residual_norm(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre=None, dst=None, eps=1e-6, Ny=None, x_out=None, y=None):
     """x [B,N,D], o [B,No,D] bf16; src, dst int32 [N] or [B,N] (None: the tokens' own order); post, pre: (gain, shift) fp32 [D] of the LayerNorms behind the branch and
     in front of the next half, or None; gate fp32 [D] or [B,D] or None -> (x_out [B,N,D], y [B,Ny,D] bf16 or None).
     x_out may be x; y: rows that dst does not name are left as they are (None: a new one, zeros there)."""
-    B, N, No, D, branch, (post_g, post_b, pre_g, pre_b), tail = _residual_step(x, o, src, post, gate, dst, pre, eps)
-    x_out = (x if o is None else torch.empty_like(x)) if x_out is None else x_out
-    _shape(x_out, x.shape, "x_out")
-    if pre is not None:
+    here, B, N, No, D, branch, norm, to = _step_arguments(x, o, src, post, gate, dst, pre)
+    px, x_out = _address(x, _BF16, here, "x"), _stream_out(x, o, x_out)
+    if pre is None:
+        Ny = 0
+    else:
         Ny = y.shape[1] if y is not None else N if Ny is None else Ny
         if y is None:
             y = x.new_empty((B, Ny, D)) if dst is None else x.new_zeros((B, Ny, D))
-        _shape(y, (B, Ny, D), "y")
-    _one_device(x_out=x_out, y=y)
+    _shape(y, (B, Ny, D), "y")
     _check("ssam_residual_norm", lib().ssam_residual_norm(
-        _bf(x, "x"), _bf(x_out, "x_out"), *branch, C.c_float(alpha), _f32(pre_g, "pre gain"), _f32(pre_b, "pre shift"), *tail, _bf(y, "y"),
-        C.c_int(B), C.c_int(N), C.c_int(No), C.c_int(Ny or 0), C.c_int(D), _stream()))
+        px, _address(x_out, _BF16, here, "x_out"), *branch, alpha, *norm, *to, eps, _address(y, _BF16, here, "y"), B, N, No, Ny, D, _stream()))
     return x_out, y
 
 
 def ssam_residual_norm_i8(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre=None, dst=None, eps=1e-6, Ny=None, x_out=None, codes=None, scales=None):
     """ssam_residual_norm with its rows in 8 bits -> (x_out, codes [B,Ny,D] int8, scales [B,Ny] fp32), the operand of ssam_linear_i8.
     codes, scales: rows that dst does not name are left as they are (None: new ones, zeros there)."""
-    B, N, No, D, branch, (post_g, post_b, pre_g, pre_b), tail = _residual_step(x, o, src, post, gate, dst, pre, eps)
-    x_out = (x if o is None else torch.empty_like(x)) if x_out is None else x_out
-    _shape(x_out, x.shape, "x_out")
+    here, B, N, No, D, branch, norm, to = _step_arguments(x, o, src, post, gate, dst, pre)
+    px, x_out = _address(x, _BF16, here, "x"), _stream_out(x, o, x_out)
     Ny = codes.shape[1] if codes is not None else scales.shape[1] if scales is not None else N if Ny is None else Ny
-    new = torch.empty if dst is None else torch.zeros
-    codes = new((B, Ny, D), dtype=torch.int8, device=x.device) if codes is None else codes
-    scales = new((B, Ny), dtype=torch.float32, device=x.device) if scales is None else scales
+    new = x.new_empty if dst is None else x.new_zeros
+    codes = new((B, Ny, D), dtype=_INT8) if codes is None else codes
+    scales = new((B, Ny), dtype=_FP32) if scales is None else scales
     _shape(codes, (B, Ny, D), "codes")
     _shape(scales, (B, Ny), "scales")
-    _one_device(x_out=x_out, codes=codes, scales=scales)
     _check("ssam_residual_norm_i8", lib().ssam_residual_norm_i8(
-        _bf(x, "x"), _bf(x_out, "x_out"), *branch, C.c_float(alpha), _f32(pre_g, "pre gain"), _f32(pre_b, "pre shift"), *tail, _dev(codes, torch.int8, "codes"),
-        _f32(scales, "scales"), C.c_int(B), C.c_int(N), C.c_int(No), C.c_int(Ny), C.c_int(D), _stream()))
+        px, _address(x_out, _BF16, here, "x_out"), *branch, alpha, *norm, *to, eps, _address(codes, _INT8, here, "codes"), _address(scales, _FP32, here, "scales"),
+        B, N, No, Ny, D, _stream()))
     return x_out, codes, scales
 
 
 def ssam_residual_norm_backward_workspace_bytes(B, N, D, gate_images=1) -> int:
-    return lib().ssam_residual_norm_backward_workspace_bytes(C.c_int(B), C.c_int(N), C.c_int(D), C.c_int(gate_images))
+    return lib().ssam_residual_norm_backward_workspace_bytes(B, N, D, gate_images)
 
 
 def ssam_residual_norm_backward(x_out, o=None, src=None, post=None, gate=None, alpha=1.0, pre=None, dst=None, eps=1e-6, dy=None, dx_out=None, dx=None, do=None,
@@ -833,29 +876,32 @@ def ssam_residual_norm_backward(x_out, o=None, src=None, post=None, gate=None, a
     """Gradients of ssam_residual_norm: x_out its stream, dy [B,Ny,D] and dx_out [B,N,D] (or None) bf16 the gradients of its results, the rest as given to it
     -> (dx, do, dgate, (dpost_g, dpost_b) or None, (dpre_g, dpre_b) or None).  dx may be dx_out; do: rows that src does not name are left as they are (None: a new one,
     zeros there)."""
-    B, N, No, D, branch, (post_g, post_b, pre_g, _), tail = _residual_step(x_out, o, src, post, gate, dst, pre, eps)
-    if pre is None and dy is not None or pre is not None and (dy is None or dy.dim() != 3):
+    here, B, N, No, D, branch, norm, to = _step_arguments(x_out, o, src, post, gate, dst, pre)
+    px = _address(x_out, _BF16, here, "x_out")
+    if (pre is None) != (dy is None):
         raise ValueError("dy: the gradient of y, where there is one")
     Ny = 0 if dy is None else dy.shape[1]
     _shape(dy, (B, Ny, D), "dy")
     dx = torch.empty_like(x_out) if dx is None else dx
     if do is None and o is not None:
         do = torch.empty_like(o) if src is None else torch.zeros_like(o)
-    for name, t, want in (("dx_out", dx_out, x_out.shape), ("dx", dx, x_out.shape), ("do", do, (B, No, D))):
-        _shape(t, want, name)
+    _shape(dx_out, x_out.shape, "dx_out")
+    _shape(dx, x_out.shape, "dx")
+    _shape(do, (B, No, D), "do")
     dgate = dpost = dpre = None
-    if weight_grads:
-        new = lambda: x_out.new_empty(D, dtype=torch.float32)  # noqa: E731
+    grads = (None, None, None, None)
+    if weight_grads and not (gate is None and post is None and pre is None):
         dgate = None if gate is None else torch.empty_like(gate)
-        dpost = None if post is None else (new(), new())
-        dpre = None if pre is None else (new(), new())
-        if workspace is None and (dgate is not None or dpost or dpre):
-            workspace = torch.empty(ssam_residual_norm_backward_workspace_bytes(B, N, D, B if gate is not None and gate.dim() == 2 else 1), dtype=torch.uint8, device=x_out.device)
-    _one_device(dy=dy, dx_out=dx_out, dx=dx, do=do, workspace=workspace)
+        grads = x_out.new_empty((4, D), dtype=_FP32).unbind(0)
+        dpost, dpre = grads[:2] if post else None, grads[2:] if pre else None
+        if workspace is None:
+            workspace = x_out.new_empty(lib().ssam_residual_norm_backward_workspace_bytes(B, N, D, B if branch[-1] else 1), dtype=_U8)
+    dpost_g, dpost_b = (grads[0].data_ptr(), grads[1].data_ptr()) if dpost else (None, None)
+    dpre_g, dpre_b = (grads[2].data_ptr(), grads[3].data_ptr()) if dpre else (None, None)
     _check("ssam_residual_norm_backward", lib().ssam_residual_norm_backward(
-        _bf(x_out, "x_out"), *branch, C.c_float(alpha), _f32(pre_g, "pre gain"), *tail, _bf(dy, "dy"), _bf(dx_out, "dx_out"), _bf(dx, "dx"), _bf(do, "do"),
-        _f32(dgate, "dgate"), *(_f32(t, "dpost") for t in dpost or (None, None)), *(_f32(t, "dpre") for t in dpre or (None, None)),
-        C.c_int(B), C.c_int(N), C.c_int(No), C.c_int(Ny), C.c_int(D), _dev(workspace, torch.uint8, "workspace"), C.c_size_t(0 if workspace is None else workspace.numel()), _stream()))
+        px, *branch, alpha, norm[0], *to, eps, _address(dy, _BF16, here, "dy"), _address(dx_out, _BF16, here, "dx_out"), _address(dx, _BF16, here, "dx"),
+        _address(do, _BF16, here, "do"), None if dgate is None else dgate.data_ptr(), dpost_g, dpost_b, dpre_g, dpre_b, B, N, No, Ny, D, _address(workspace, _U8, here, "workspace"),
+        0 if workspace is None else workspace.numel(), _stream()))
     return dx, do, dgate, dpost, dpre
 
 

@@ -94,15 +94,6 @@ __device__ __forceinline__ void gemm_warm(const GemmWarm &warm, int group)
     }
 }
 
-// Sum over the four quads of a wave's lanes.
-__device__ __forceinline__ float gemm_quad_sum(float v)
-{
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    const float s = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(s), __float_as_uint(s), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-
 // PARTS: the row statistics of the folded LayerNorm come in pieces (GemmParts), or, of a scatter-add, it leaves such pieces.
 // The pieces of a tile's rows are as large as a slab of A and come as one more, into the stage that the last slab but SA - 1 has freed: no registers, and
 // under the products of the last slabs.  Loaded in front of the ring's first slabs they cost 4 us, as much as the launch they save.

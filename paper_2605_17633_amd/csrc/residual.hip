@@ -1,6 +1,8 @@
 // The step between two halves of a block, forward and backward, and rows in 8 bits: the branch behind its own LayerNorm and a gate joins the scaled residual
 // stream, whose LayerNorm goes to the rows that the next half reads, in bf16 or in 8 bits.  All of it is bound by HBM: one pass over the data, 16 bytes of bf16 per
 // lane and request.
+#include <type_traits>
+
 #include "rows8.h"
 
 namespace {
@@ -46,7 +48,7 @@ struct Chunks {
         const float4 lo = reinterpret_cast<const float4 *>(p)[2 * at[i]], hi = reinterpret_cast<const float4 *>(p)[2 * at[i] + 1];
         v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
     }
-    // v -> (v - mean) / deviation; returns one over the deviation.  Two passes over the registers, fp32.
+    // v -> (v - mean) / deviation, zeros past the row; returns one over the deviation.  Two passes over the registers, fp32.
     __device__ __forceinline__ float normalise(float (&v)[MAXC][8], float eps) const
     {
         float s = 0.f, q = 0.f;
@@ -54,35 +56,17 @@ struct Chunks {
         for (int i = 0; i < MAXC; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) s += in[i] ? v[i][e] : 0.f;
-        const float mean = wave_sum(s) * over_D;
+        const float mean = lanes_sum(s) * over_D;
 #pragma unroll
         for (int i = 0; i < MAXC; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { v[i][e] -= mean; q += in[i] ? v[i][e] * v[i][e] : 0.f; }
-        const float rstd = rsqrtf(wave_sum(q) * over_D + eps);
+            for (int e = 0; e < 8; ++e) { v[i][e] = in[i] ? v[i][e] - mean : 0.f; q = fmaf(v[i][e], v[i][e], q); }
+        const float rstd = rsqrtf(lanes_sum(q) * over_D + eps);
 #pragma unroll
         for (int i = 0; i < MAXC; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] *= rstd;
         return rstd;
-    }
-    // The gradient of normalise: g -> rstd (g - mean(g) - h mean(g h))
-    __device__ __forceinline__ void normalise_back(float (&g)[MAXC][8], const float (&h)[MAXC][8], float rstd) const
-    {
-        float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-        for (int i = 0; i < MAXC; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                s1 += in[i] ? g[i][e] : 0.f;
-                s2 += in[i] ? g[i][e] * h[i][e] : 0.f;
-            }
-        s1 = wave_sum(s1) * over_D;
-        s2 = wave_sum(s2) * over_D;
-#pragma unroll
-        for (int i = 0; i < MAXC; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) g[i][e] = rstd * (g[i][e] - s1 - h[i][e] * s2);
     }
 };
 
@@ -183,8 +167,7 @@ residual_norm_kernel(StepArgs a)
             for (int i = 0; i < MAXC; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7fffffffu);
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+            top = lanes_max(top);
             const bool finite = top < 0x7f800000u;
             const RowScale s = row_scale(finite ? __uint_as_float(top) : 0.f);
 #pragma unroll
@@ -214,10 +197,10 @@ int launch_step(const StepArgs &a, bool post, StepOut out, hipStream_t st)
 // ---------------------------------------------------------------- backward
 // A token's G = dx_out + gradient of the second LayerNorm is all that the rest needs, and stays in registers:
 //   dx = alpha G (G without a branch),  dn = gate G,  do = gradient of the first LayerNorm (dn).
-// The weights' gradients come from sums over tokens of at most four vectors: G, G h, dy h_x and dy (h, h_x: the normalised rows; h = o without a first LayerNorm):
+// The weights' gradients come from sums over tokens of at most four vectors: G h, G, dy h_x and dy (h, h_x: the normalised rows; h = o without a first LayerNorm):
 //   dgate = post_g sum(G h) + post_b sum(G) or sum(G o),  dpost_g = gate sum(G h),  dpost_b = gate sum(G);  with a gate of every image the first two are summed per image.
-// Waves walk the tokens and keep their share of the sums in registers; the four waves of a workgroup add theirs up in LDS, a second launch adds
-// the workgroups' up, a third the images', all in a fixed order: no atomics, the same bits every time.
+// Waves walk the tokens and keep their share of the sums, two vectors in registers and the others in LDS (all four in registers leave one wave to a SIMD, under whose arithmetic
+// nothing is requested); the eight waves of a workgroup add theirs up, a second launch adds the workgroups' up, a third the images', all in a fixed order: no atomics, the same bits every time.
 struct BackArgs {
     const uint4 *x_out, *o, *dy, *dx_out;
     uint4 *dx, *d_o;
@@ -225,128 +208,221 @@ struct BackArgs {
     const float *post_g, *gate, *pre_g;
     int gate_stride;
     float alpha, eps;
-    float *parts;                             // [images or 1][workgroups][NV][D]
-    int tokens, N, chunks;                    // tokens: of a group (gridDim.y groups)
+    float *parts;                             // [groups][workgroups][NV][D]
+    int tokens, N, chunks;                    // tokens: of a group (gridDim.y groups: images where the gate is of every image)
 };
 
-// Sums of a launch: vectors of them, and where each is
+// Sums of a launch: vectors of them, and where each is; the first LDS of them are in LDS
 template <bool POST, bool PRE>
 struct Sums {
-    static constexpr int GH = 0, G = 1, DYH = 1 + POST, DY = 2 + POST, NV = 1 + POST + 2 * PRE;
+    static constexpr int GH = 0, G = 1, DYH = 1 + POST, DY = 2 + POST, NV = 1 + POST + 2 * PRE, IN_REGISTERS = NV < 2 ? NV : 2, IN_LDS = NV - IN_REGISTERS;
 };
 
+// Waves of a workgroup, one to a CU.  Rows above 1536 with both norms spill 67 of the 256 registers that two waves to a SIMD have.
+constexpr int back_waves(int maxc) { return maxc == 4 ? 4 : 8; }
+
+// LDS of a workgroup: both norms' factors, and the waves' sums, or room for a vector of all of them
+template <bool POST, bool PRE, bool WEIGHTS>
+constexpr size_t backward_lds(int maxc)
+{
+    const int vectors = Sums<POST, PRE>::IN_LDS > 1 ? Sums<POST, PRE>::IN_LDS : 1;
+    return sizeof(float4) * 128 * maxc * (2 + (WEIGHTS ? back_waves(maxc) * vectors : 0));
+}
+
 template <int MAXC, bool POST, bool PRE, bool WEIGHTS>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(64 * back_waves(MAXC))
 residual_norm_backward_kernel(BackArgs a)
 {
     using V = Sums<POST, PRE>;
-    __shared__ float4 lds[WEIGHTS ? WAVES * 64 * 2 : 1];
+    extern __shared__ float4 lds4[];              // [2][2 MAXC][64] factors, then [wave][IN_LDS][2 MAXC][64]: halves of a lane's chunks, lanes side by side
+    constexpr int VECTOR = 2 * MAXC * 64, BACK_WAVES = back_waves(MAXC);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const Chunks<MAXC> ch(a.chunks);
-    float sums[WEIGHTS ? V::NV : 1][MAXC][8];
-    if constexpr (WEIGHTS)
+    const float *gate = a.gate ? a.gate + (long)blockIdx.y * a.gate_stride : nullptr;
+    float4 *const mine = lds4 + 2 * VECTOR + wave * (V::IN_LDS * VECTOR) + lane;
+    // factors: of the second LayerNorm its gain, of the branch the gate times the first one's; zeros past the row
+    for (int k = threadIdx.x; k < VECTOR; k += 64 * BACK_WAVES) {
+        const int c = (k & 63) + 64 * (k >> 7), quad = 2 * c + ((k >> 6) & 1);
+        const bool in = c < a.chunks;
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f), w = f;
+        if (in && PRE) f = reinterpret_cast<const float4 *>(a.pre_g)[quad];
+        if (in) {
+            w = gate ? reinterpret_cast<const float4 *>(gate)[quad] : make_float4(1.f, 1.f, 1.f, 1.f);
+            if constexpr (POST) {
+                const float4 g = reinterpret_cast<const float4 *>(a.post_g)[quad];
+                w.x *= g.x; w.y *= g.y; w.z *= g.z; w.w *= g.w;
+            }
+        }
+        lds4[k] = f;
+        lds4[VECTOR + k] = w;
+    }
+    float regs[WEIGHTS ? V::IN_REGISTERS : 1][MAXC][8];
+    if constexpr (WEIGHTS) {
 #pragma unroll
-        for (int w = 0; w < V::NV; ++w)
+        for (int w = 0; w < V::IN_REGISTERS; ++w)
 #pragma unroll
             for (int i = 0; i < MAXC; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sums[w][i][e] = 0.f;
-    for (int r = blockIdx.x * WAVES + wave; r < a.tokens; r += gridDim.x * WAVES) {
-        const int row = blockIdx.y * a.tokens + r, b = row / a.N, t = row - b * a.N;
-        const int p = a.rows.branch(b, t), q = PRE ? a.rows.out(b, t) : -1;
-        const long at = (long)row * a.chunks, branch = ((long)b * a.rows.No + p) * a.chunks;
-        uint4 rg[MAXC], ro[MAXC], rx[MAXC], ry[MAXC];
-        if (a.dx_out) ch.load(a.dx_out + at, rg);
-        if (p >= 0) ch.load(a.o + branch, ro);
-        if (PRE && q >= 0) {
+                for (int e = 0; e < 8; ++e) regs[w][i][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < V::IN_LDS * 2 * MAXC; ++k) mine[k * 64] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __syncthreads();
+    auto factors = [&](int which, int i, float (&f)[8]) {
+        const float4 lo = lds4[which * VECTOR + i * 128 + lane], hi = lds4[which * VECTOR + i * 128 + 64 + lane];
+        f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w; f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
+    };
+    // sums of vector v (of lanes past the row they are never stored) += t * u
+    auto add = [&](auto v_, int i, const float (&t)[8], const float (&u)[8]) {
+        constexpr int v = decltype(v_)::value;
+        if constexpr (v >= V::IN_LDS) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) regs[v - V::IN_LDS][i][e] = fmaf(t[e], u[e], regs[v - V::IN_LDS][i][e]);
+        } else {
+            float4 *p = mine + v * VECTOR + i * 128;
+            float4 lo = p[0], hi = p[64];
+            lo.x = fmaf(t[0], u[0], lo.x); lo.y = fmaf(t[1], u[1], lo.y); lo.z = fmaf(t[2], u[2], lo.z); lo.w = fmaf(t[3], u[3], lo.w);
+            hi.x = fmaf(t[4], u[4], hi.x); hi.y = fmaf(t[5], u[5], hi.y); hi.z = fmaf(t[6], u[6], hi.z); hi.w = fmaf(t[7], u[7], hi.w);
+            p[0] = lo;
+            p[64] = hi;
+        }
+    };
+    using std::integral_constant;
+    constexpr float ONES[8] = { 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f };
+
+    const int stride = gridDim.x * BACK_WAVES;
+    struct Token { int row, p, q; long branch, out; };         // p, q < 0: no branch, no row of y
+    auto token = [&](int r) {
+        Token t = { -1, -1, -1, 0, 0 };
+        if (r >= a.tokens) return t;
+        t.row = blockIdx.y * a.tokens + r;
+        const int b = t.row / a.N, at = t.row - b * a.N;
+        t.p = a.rows.branch(b, at);
+        t.q = PRE ? a.rows.out(b, at) : -1;
+        t.branch = ((long)b * a.rows.No + t.p) * a.chunks;
+        t.out = ((long)b * a.rows.Ny + t.q) * a.chunks;
+        return t;
+    };
+    uint4 rg[MAXC], ro[MAXC], rx[MAXC], ry[MAXC];
+    auto request = [&](const Token &t) {
+        if (t.row < 0) return;
+        const long at = (long)t.row * a.chunks;
+        if (PRE && t.q >= 0) {
             ch.load(a.x_out + at, rx);
-            ch.load(a.dy + ((long)b * a.rows.Ny + q) * a.chunks, ry);
+            ch.load(a.dy + t.out, ry);
         }
-        float g[MAXC][8];
-#pragma unroll
-        for (int i = 0; i < MAXC; ++i) {
-            if (!a.dx_out) rg[i] = make_uint4(0, 0, 0, 0);
-            unpack_bf16x8(rg[i], g[i]);
-        }
-        if (PRE && q >= 0) {
-            float h[MAXC][8], d[MAXC][8];
-            ch.unpack(rx, h);
-            ch.unpack(ry, d);
-            const float rstd = ch.normalise(h, a.eps);
-#pragma unroll
-            for (int i = 0; i < MAXC; ++i) {
-                float w[8];
-                ch.values(a.pre_g, i, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if constexpr (WEIGHTS && PRE) {          // of lanes past the row these are never stored
-                        sums[V::DYH][i][e] = fmaf(d[i][e], h[i][e], sums[V::DYH][i][e]);
-                        sums[V::DY][i][e] += d[i][e];
-                    }
-                    d[i][e] *= w[e];
-                }
-            }
-            ch.normalise_back(d, h, rstd);
+        if (a.dx_out) ch.load(a.dx_out + at, rg);
+        if (t.p >= 0) ch.load(a.o + t.branch, ro);
+    };
+    int r = blockIdx.x * BACK_WAVES + wave;
+    Token now = token(r), next = token(r + stride);            // (tokens + 2 strides stay below 2^31)
+    request(now);
+    for (; r < a.tokens; r += stride) {
+        float g[MAXC][8], h[MAXC][8], d[MAXC][8], o[MAXC][8];
+        ch.unpack(rg, g);
+        ch.unpack(rx, h);
+        ch.unpack(ry, d);
+        ch.unpack(ro, o);
+        // the next token's rows, and the token behind it: their round trips are under this one's arithmetic
+        const Token t = now;
+        request(next);
+        now = next;
+        next = token(r + 2 * stride);
+        if (!a.dx_out) {
 #pragma unroll
             for (int i = 0; i < MAXC; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[i][e] += d[i][e];
+                for (int e = 0; e < 8; ++e) g[i][e] = 0.f;
         }
-        if (p >= 0) {
-            float h[MAXC][8], d[MAXC][8];
-            ch.unpack(ro, h);
-            float rstd = 1.f;
-            if constexpr (POST) rstd = ch.normalise(h, a.eps);
+        if (PRE && t.q >= 0) {
+            const float rstd = ch.normalise(h, a.eps);
+            float s1 = 0.f, s2 = 0.f;
 #pragma unroll
             for (int i = 0; i < MAXC; ++i) {
-                float w[8];
+                float f[8];
+                factors(0, i, f);
+                if constexpr (WEIGHTS && PRE) {
+                    add(integral_constant<int, V::DYH>{}, i, d[i], h[i]);
+                    add(integral_constant<int, V::DY>{}, i, d[i], ONES);
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    if constexpr (WEIGHTS) {
-                        sums[V::GH][i][e] = fmaf(g[i][e], h[i][e], sums[V::GH][i][e]);
-                        if constexpr (POST) sums[V::G][i][e] += g[i][e];
-                    }
-                    d[i][e] = g[i][e];
-                    g[i][e] *= a.alpha;
-                }
-                if (a.gate) {
-                    ch.values(a.gate + (long)b * a.gate_stride, i, w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) d[i][e] *= w[e];
-                }
-                if constexpr (POST) {
-                    ch.values(a.post_g, i, w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) d[i][e] *= w[e];
+                    d[i][e] *= f[e];
+                    s1 += d[i][e];
+                    s2 = fmaf(d[i][e], h[i][e], s2);
                 }
             }
-            if constexpr (POST) ch.normalise_back(d, h, rstd);
-            ch.store(a.d_o + branch, d);
+            s1 = lanes_sum(s1) * ch.over_D;
+            s2 = lanes_sum(s2) * ch.over_D;
+#pragma unroll
+            for (int i = 0; i < MAXC; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[i][e] = fmaf(rstd, fmaf(-h[i][e], s2, d[i][e] - s1), g[i][e]);
         }
-        ch.store(a.dx + at, g);
+        if (t.p >= 0) {
+            float rstd = 1.f, s1 = 0.f, s2 = 0.f;
+            if constexpr (POST) rstd = ch.normalise(o, a.eps);
+#pragma unroll
+            for (int i = 0; i < MAXC; ++i) {
+                float f[8];
+                factors(1, i, f);
+                if constexpr (WEIGHTS) {
+                    add(integral_constant<int, V::GH>{}, i, g[i], o[i]);
+                    if constexpr (POST) add(integral_constant<int, V::G>{}, i, g[i], ONES);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    d[i][e] = g[i][e] * f[e];
+                    g[i][e] *= a.alpha;
+                    if constexpr (POST) {
+                        s1 += d[i][e];
+                        s2 = fmaf(d[i][e], o[i][e], s2);
+                    }
+                }
+            }
+            if constexpr (POST) {
+                s1 = lanes_sum(s1) * ch.over_D;
+                s2 = lanes_sum(s2) * ch.over_D;
+#pragma unroll
+                for (int i = 0; i < MAXC; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[i][e] = rstd * fmaf(-o[i][e], s2, d[i][e] - s1);
+            }
+            ch.store(a.d_o + t.branch, d);
+        }
+        ch.store(a.dx + (long)t.row * a.chunks, g);
     }
     if constexpr (WEIGHTS) {
-        // the waves' sums of 8 columns at a time, [wave][which half][lane]: every lane then adds up one float4 of four waves
-        float *mine = a.parts + ((long)blockIdx.y * gridDim.x + blockIdx.x) * V::NV * a.chunks * 8;
+        // the waves' sums, a vector at a time: those in LDS, then those of the registers in their place
+        float4 *const all = lds4 + 2 * VECTOR;
+        float4 *const out = reinterpret_cast<float4 *>(a.parts) + ((long)blockIdx.y * gridDim.x + blockIdx.x) * V::NV * (2 * a.chunks);
+        auto reduce = [&](int vector, int at, int pitch) {
+            for (int k = threadIdx.x; k < VECTOR; k += 64 * BACK_WAVES) {
+                const int c = (k & 63) + 64 * (k >> 7);
+                float4 s = all[at + k];
 #pragma unroll
-        for (int i = 0; i < MAXC; ++i)
-#pragma unroll
-            for (int w = 0; w < V::NV; ++w) {
-                const float *f = sums[w][i];
-                __syncthreads();
-                lds[(wave * 2 + 0) * 64 + lane] = make_float4(f[0], f[1], f[2], f[3]);
-                lds[(wave * 2 + 1) * 64 + lane] = make_float4(f[4], f[5], f[6], f[7]);
-                __syncthreads();
-                if (wave < 2 && ch.in[i]) {
-                    float4 s = lds[wave * 64 + lane];
-#pragma unroll
-                    for (int o = 1; o < WAVES; ++o) {
-                        const float4 t = lds[(o * 2 + wave) * 64 + lane];
-                        s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
-                    }
-                    reinterpret_cast<float4 *>(mine + (long)w * a.chunks * 8)[2 * (lane + 64 * i) + wave] = s;
+                for (int w = 1; w < BACK_WAVES; ++w) {
+                    const float4 t = all[w * pitch + at + k];
+                    s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
                 }
+                if (c < a.chunks) out[(long)vector * 2 * a.chunks + 2 * c + ((k >> 6) & 1)] = s;
             }
+        };
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V::IN_LDS; ++v) reduce(v, v * VECTOR, V::IN_LDS * VECTOR);
+#pragma unroll
+        for (int v = 0; v < V::IN_REGISTERS; ++v) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < MAXC; ++i) {
+                const float *f = regs[v][i];
+                all[wave * VECTOR + i * 128 + lane] = make_float4(f[0], f[1], f[2], f[3]);
+                all[wave * VECTOR + i * 128 + 64 + lane] = make_float4(f[4], f[5], f[6], f[7]);
+            }
+            __syncthreads();
+            reduce(V::IN_LDS + v, 0, VECTOR);
+        }
     }
 }
 
@@ -360,101 +436,100 @@ struct WeightGrads {
 __device__ __forceinline__ float4 mul4(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
 __device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 
-// The sums of a group of tokens, of four columns -> the gradients
-template <bool POST, bool PRE>
-__device__ __forceinline__ void gate_gradient(const WeightGrads &w, int image, int quad, const float4 *s)
+// Sums over rows of parts, of the two vectors from `first` on and four columns: eight lanes with 16 bytes each, 32 slices of the rows, eight of them in a wave.  What slice 0 of wave 0 gets is whole.
+template <int NV, int VECTORS>
+__device__ __forceinline__ void sum_of_rows(const float4 *parts, int rows, int first, int quads, int quad, float4 (&s)[VECTORS])
 {
-    using V = Sums<POST, PRE>;
-    float4 d = s[V::GH];
-    if constexpr (POST) d = add4(mul4(reinterpret_cast<const float4 *>(w.post_g)[quad], s[V::GH]), mul4(reinterpret_cast<const float4 *>(w.post_b)[quad], s[V::G]));
-    if (w.dgate) reinterpret_cast<float4 *>(w.dgate + (long)image * w.D)[quad] = d;
+    __shared__ float4 lds[3][VECTORS][8];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 7;
+#pragma unroll
+    for (int k = 0; k < VECTORS; ++k) s[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int r = threadIdx.x >> 3; r < rows; r += 32)
+#pragma unroll
+        for (int k = 0; k < VECTORS; ++k) s[k] = add4(s[k], parts[((long)r * NV + first + k) * quads + quad]);
+    auto slices = [](float v) { v += rotate16<8>(v); return gemm_quad_sum(v); };
+#pragma unroll
+    for (int k = 0; k < VECTORS; ++k) {
+        s[k] = make_float4(slices(s[k].x), slices(s[k].y), slices(s[k].z), slices(s[k].w));
+        if (wave > 0 && lane < 8) lds[wave - 1][k][c] = s[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < VECTORS; ++k)
+#pragma unroll
+        for (int w = 0; w < 3; ++w) s[k] = add4(s[k], lds[w][k][c]);
 }
 
-template <bool POST, bool PRE>
-__device__ __forceinline__ void norm_gradients(const WeightGrads &w, int quad, const float4 *s)      // s: the gate is in it
-{
-    using V = Sums<POST, PRE>;
-    auto put = [&](float *to, const float4 &v) { if (to) reinterpret_cast<float4 *>(to)[quad] = v; };
-    if constexpr (POST) { put(w.dpost_g, s[V::GH]); put(w.dpost_b, s[V::G]); }
-    if constexpr (PRE) { put(w.dpre_g, s[V::DYH]); put(w.dpre_b, s[V::DY]); }
-}
+__device__ __forceinline__ void put4(float *to, int quad, const float4 &v) { if (to) reinterpret_cast<float4 *>(to)[quad] = v; }
 
-template <bool POST, bool PRE>
-__device__ __forceinline__ void times_gate(const WeightGrads &w, int image, int quad, float4 *s)
-{
-    using V = Sums<POST, PRE>;
-    if (!POST || !w.gate) return;
-    const float4 g = reinterpret_cast<const float4 *>(w.gate + (long)image * w.gate_stride)[quad];
-    s[V::GH] = mul4(s[V::GH], g);
-    if constexpr (POST) s[V::G] = mul4(s[V::G], g);
-}
-
-// [groups][n][NV][D] -> sums over n.  A workgroup adds up 32 columns of a group: eight lanes with 16 bytes each, 32 slices of the rows.  One group: the gradients; more: the
-// gate's of the group, and its sums, gate in them, to `images` [groups][NV][D].
+// parts [groups][n][NV][D] -> the gradients, 32 columns a workgroup.  blockIdx.z 0: of the branch (vectors G h and G) in group blockIdx.y; of many groups the LayerNorm's, gate in them, go to
+// `images` [groups][2][D] instead.  1: of the second LayerNorm, over all groups.
 template <bool POST, bool PRE>
 __global__ void __launch_bounds__(256)
 residual_weight_sums_kernel(const float4 *__restrict__ parts, int n, WeightGrads w, float4 *images)
 {
-    constexpr int NV = Sums<POST, PRE>::NV;
-    __shared__ float4 lds[256];
-    const int c = threadIdx.x & 7, slice = threadIdx.x >> 3, quads = w.D / 4, quad = blockIdx.x * 8 + c, at = min(quad, quads - 1), group = blockIdx.y;
-    parts += (long)group * n * NV * quads;
-    float4 s[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) s[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int r = slice; r < n; r += 32)
-#pragma unroll
-        for (int k = 0; k < NV; ++k) s[k] = add4(s[k], parts[((long)r * NV + k) * quads + at]);
-#pragma unroll
-    for (int k = 0; k < NV; ++k) s[k] = sum_of_shares(s[k], lds);
-    if (slice != 0 || quad >= quads) return;
-    gate_gradient<POST, PRE>(w, group, quad, s);
-    times_gate<POST, PRE>(w, group, quad, s);
-    if (gridDim.y == 1) {
-        norm_gradients<POST, PRE>(w, quad, s);
+    using V = Sums<POST, PRE>;
+    const int quads = w.D / 4, quad = blockIdx.x * 8 + (threadIdx.x & 7), at = min(quad, quads - 1), group = blockIdx.y;
+    const bool whole = threadIdx.x < 8 && quad < quads;
+    if constexpr (PRE) if (blockIdx.z == 1) {
+        if (group != 0) return;
+        float4 s[2];
+        sum_of_rows<V::NV>(parts, n * gridDim.y, V::DYH, quads, at, s);
+        if (whole) { put4(w.dpre_g, quad, s[0]); put4(w.dpre_b, quad, s[1]); }
         return;
     }
-#pragma unroll
-    for (int k = 0; k < NV; ++k) images[((long)group * NV + k) * quads + quad] = s[k];
+    float4 s[1 + POST];
+    sum_of_rows<V::NV>(parts + (long)group * n * V::NV * quads, n, V::GH, quads, at, s);
+    if (!whole) return;
+    float4 d = s[0];
+    if constexpr (POST) d = add4(mul4(reinterpret_cast<const float4 *>(w.post_g)[quad], s[0]), mul4(reinterpret_cast<const float4 *>(w.post_b)[quad], s[1]));
+    put4(w.dgate ? w.dgate + (long)group * w.D : nullptr, quad, d);
+    if constexpr (POST) {
+        if (w.gate) {
+            const float4 g = reinterpret_cast<const float4 *>(w.gate + (long)group * w.gate_stride)[quad];
+            s[0] = mul4(s[0], g);
+            s[1] = mul4(s[1], g);
+        }
+        if (gridDim.y == 1) { put4(w.dpost_g, quad, s[0]); put4(w.dpost_b, quad, s[1]); }
+        else { images[(long)group * 2 * quads + quad] = s[0]; images[((long)group * 2 + 1) * quads + quad] = s[1]; }
+    }
 }
 
-template <bool POST, bool PRE>
-__global__ void __launch_bounds__(64)
+// images [groups][2][D] -> the sums over groups, as above
+__global__ void __launch_bounds__(256)
 residual_image_sums_kernel(const float4 *__restrict__ images, int groups, WeightGrads w)
 {
-    constexpr int NV = Sums<POST, PRE>::NV;
-    const int quads = w.D / 4, quad = blockIdx.x * 64 + threadIdx.x;
-    if (quad >= quads) return;
-    float4 s[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) s[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int g = 0; g < groups; ++g)
-#pragma unroll
-        for (int k = 0; k < NV; ++k) s[k] = add4(s[k], images[((long)g * NV + k) * quads + quad]);
-    norm_gradients<POST, PRE>(w, quad, s);
+    const int quads = w.D / 4, quad = blockIdx.x * 8 + (threadIdx.x & 7);
+    float4 s[2];
+    sum_of_rows<2>(images, groups, 0, quads, min(quad, quads - 1), s);
+    if (threadIdx.x < 8 && quad < quads) { put4(w.dpost_g, quad, s[0]); put4(w.dpost_b, quad, s[1]); }
 }
 
-// Workgroups that a group of tokens is dealt to: two waves to a SIMD of 256 CUs over all groups.
-inline int backward_workgroups(long tokens, int groups)
+// Workgroups that a group of tokens is dealt to: one to a CU over all groups.
+inline int backward_workgroups(long tokens, int groups, int maxc)
 {
-    const long most = ssam_div_up(512, groups), need = (tokens + WAVES - 1) / WAVES;
+    const long most = ssam_div_up(256, groups), need = (tokens + back_waves(maxc) - 1) / back_waves(maxc);
     return (int)(need < most ? need : most);
 }
 
 template <int MAXC, bool POST, bool PRE>
 int launch_backward(const BackArgs &a, const WeightGrads &w, bool weights, int groups, hipStream_t st)
 {
-    const int n = backward_workgroups(a.tokens, groups);
+    const int n = backward_workgroups(a.tokens, groups, MAXC);
     const dim3 grid(n, groups);
-    hipLaunchKernelGGL((weights ? residual_norm_backward_kernel<MAXC, POST, PRE, true> : residual_norm_backward_kernel<MAXC, POST, PRE, false>), grid, dim3(64 * WAVES), 0, st, a);
+    auto kern = weights ? residual_norm_backward_kernel<MAXC, POST, PRE, true> : residual_norm_backward_kernel<MAXC, POST, PRE, false>;
+    const size_t lds = weights ? backward_lds<POST, PRE, true>(MAXC) : backward_lds<POST, PRE, false>(MAXC);
+    // more than 64 KiB of LDS per workgroup needs the per-kernel opt-in (idempotent, host-side only)
+    if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return SSAM_EHIP;
+    hipLaunchKernelGGL(kern, grid, dim3(64 * back_waves(MAXC)), lds, st, a);
     SSAM_CHECK_LAUNCH();
     if (!weights) return SSAM_OK;
     float4 *images = reinterpret_cast<float4 *>(a.parts + (size_t)groups * n * Sums<POST, PRE>::NV * w.D);
-    hipLaunchKernelGGL((residual_weight_sums_kernel<POST, PRE>), dim3(ssam_div_up(w.D, 32), groups), dim3(256), 0, st, (const float4 *)a.parts, n, w, images);
+    hipLaunchKernelGGL((residual_weight_sums_kernel<POST, PRE>), dim3(ssam_div_up(w.D, 32), groups, 1 + PRE), dim3(256), 0, st, (const float4 *)a.parts, n, w, images);
     SSAM_CHECK_LAUNCH();
-    if (groups > 1) {
-        hipLaunchKernelGGL((residual_image_sums_kernel<POST, PRE>), dim3(ssam_div_up(w.D, 256)), dim3(64), 0, st, (const float4 *)images, groups, w);
+    if (POST && groups > 1) {
+        hipLaunchKernelGGL(residual_image_sums_kernel, dim3(ssam_div_up(w.D, 32)), dim3(256), 0, st, (const float4 *)images, groups, w);
         SSAM_CHECK_LAUNCH();
     }
     return SSAM_OK;
@@ -488,9 +563,7 @@ quantize_rows_kernel(const uint4 *__restrict__ x, uint2 *__restrict__ codes, flo
     } else {
         for (int c = lane; c < chunks; c += 64) top = max_u16x2(top, top_of_bf16x8(x[c]));
     }
-    top = max(top >> 16, top & 0xffffu);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    top = lanes_max(max(top >> 16, top & 0xffffu));
     const bool finite = top < 0x7f80u;
     const RowScale s = row_scale(finite ? bf16_bits_to_float(top) : 0.f);
     auto put = [&](int c, const uint4 &r) {
@@ -594,8 +667,8 @@ extern "C" int ssam_residual_norm_i8(const void *x, void *x_out, const void *o, 
 
 extern "C" size_t ssam_residual_norm_backward_workspace_bytes(int B, int N, int D, int gate_images)
 {
-    if (B <= 0 || N <= 0 || D <= 0 || (gate_images != 1 && gate_images != B)) return 0;
-    const int n = backward_workgroups(gate_images == 1 ? (long)B * N : N, gate_images);
+    if (B <= 0 || N <= 0 || D <= 0 || D > 2048 || (gate_images != 1 && gate_images != B)) return 0;
+    const int n = backward_workgroups(gate_images == 1 ? (long)B * N : N, gate_images, ssam_div_up(D, 512));
     return (size_t)gate_images * (n + (gate_images > 1)) * 4 * D * sizeof(float);
 }
 
@@ -611,16 +684,16 @@ extern "C" int ssam_residual_norm_backward(const void *x_out, const void *o, con
     if (int rc = check_step(o, src, src_batch_stride, post_g, post_b, gate, gate_batch_stride, pre_g, dst, dst_batch_stride, B, N, No, Ny, D); rc != SSAM_OK) return rc;
     const bool weights = dgate || dpost_g || dpost_b || dpre_g || dpre_b;
     const int groups = gate && gate_batch_stride ? B : 1;
+    if (groups > 65535) return SSAM_EUNSUPPORTED;                      // gridDim.y
     if (weights) {
-        if (groups > 65535) return SSAM_EUNSUPPORTED;                  // gridDim.y
         if (!workspace || !ssam_aligned16(workspace)) return SSAM_EINVAL;
         if (workspace_bytes < ssam_residual_norm_backward_workspace_bytes(B, N, D, groups)) return SSAM_EWORKSPACE;
     }
     const TokenRows rows = { src, dst, src_batch_stride, dst_batch_stride, o ? No : 0, pre_g ? Ny : 0 };
     const BackArgs a = { (const uint4 *)x_out, (const uint4 *)o, (const uint4 *)dy, (const uint4 *)dx_out, (uint4 *)dx, (uint4 *)d_o, rows, post_g, gate, pre_g,
-                         gate_batch_stride, alpha, eps, (float *)workspace, weights && groups > 1 ? N : B * N, N, D / 8 };
+                         gate_batch_stride, alpha, eps, (float *)workspace, groups > 1 ? N : B * N, N, D / 8 };
     const WeightGrads w = { post_g, post_b, gate, gate_batch_stride, dgate, dpost_g, dpost_b, dpre_g, dpre_b, D };
     const int maxc = ssam_div_up(D / 8, 64);
     auto go = maxc == 1 ? launch_backward<1> : maxc == 2 ? launch_backward<2> : maxc == 3 ? launch_backward<3> : launch_backward<4>;
-    return go(a, w, post_g != nullptr, pre_g != nullptr, weights, weights ? groups : 1, (hipStream_t)stream);
+    return go(a, w, post_g != nullptr, pre_g != nullptr, weights, groups, (hipStream_t)stream);
 }
