@@ -38,24 +38,18 @@ __device__ __forceinline__ int gemm_i8_row(const GemmI8Args &a, int m)
     return (unsigned)idx < (unsigned)a.rm.dst_rows_per_batch ? b * a.rm.dst_rows_per_batch + idx : -1;
 }
 
+// The workgroup's tile from row m0 and column n0 on.
 template <int BM, int BN, int WGK, int EPI>
-__global__ void __launch_bounds__(512, 1)
-gemm_i8_wide_kernel(GemmI8Args a, GemmTileRange tr)
+__device__ __forceinline__ void gemm_i8_tile(const GemmI8Args &a, int m0, int n0, unsigned char *smem)
 {
     using G = GemmWide<BM, BN, WGK>;
     constexpr int WGN = G::WGN, MT = G::MT, NT = G::NT, NP = NT / 2, WM = MT * 16, WN = NT * 16, SA = G::SA, SW = G::SW, L = G::L;
-    constexpr bool ADD = EPI == SSAM_EPI_BIAS_SCATTER_ADD, EARLY = MT * NT < 24;       // registers for what the epilogue reads before the last slabs
+    constexpr bool ADD = EPI == SSAM_EPI_BIAS_SCATTER_ADD, EARLY = MT * NT < 24 && !(ADD && WGK == 2 && NT == 3);       // registers for what the epilogue reads before the last slabs
     static_assert(!EARLY || G::EARLY, "and LDS for the row map");
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     // WGK == 1: SA slabs of A, then SW of W; 2: slab by slab, A then W
     constexpr int STRIDE_A = WGK == 1 ? G::AB : G::AB + G::WB, STRIDE_W = WGK == 1 ? G::WB : G::AB + G::WB, W0 = WGK == 1 ? SA * G::AB : G::AB;
     unsigned char *as = smem, *ws = smem + W0;
     using std::integral_constant;
-
-    const int per_xcd = (tr.tile_count + 7) / 8, tl = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if (tl >= tr.tile_count) return;
-    int m0, n0;
-    gemm_tile_origin(tr, tl, 0, 1, 1, BM, BN, m0, n0);
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wk = wave * WGK >> 3, wt = wave & (8 / WGK - 1), wm = wt / WGN * WM, wn = wt % WGN * WN;
@@ -157,14 +151,31 @@ gemm_i8_wide_kernel(GemmI8Args a, GemmTileRange tr)
     int drow[MTH];                                // destination rows, -1: not stored
     float rs[MTH];
     f32x4 bv[NB], cs[NB];
-    constexpr int ROW = NP * 4 + NT % 2 * 2, AHEAD = !ADD ? 1 : ROW * MTH <= 32 ? MTH : 32 / ROW;      // rows whose old values are requested ahead
-    uint4 old[ADD ? AHEAD : 1][NP > 0 ? NP : 1];
-    uint2 old1[ADD ? AHEAD : 1];
-    auto load_old = [&](int k) {
-        const bf16 *row = a.C + (long)max(drow[k], 0) * a.ld.c;      // a row that is not stored reads row 0 and drops the value
+    // Results go to memory through LDS, where lanes that follow each other take 16 bytes that follow each other: slot (row, chunk of 8 columns) = lane + 64 j of GK * 16 rows.  Straight from the
+    // accumulators 16 lanes write 16 rows, 16 bytes each.
+    constexpr int CH = 2 * NT, GK = NT == 3 ? 2 : 1, J = GK * 16 * CH / 64, PITCH = CH * (ADD ? 32 : 16) + 16;
+    static_assert(GK * 16 * CH % 64 == 0 && MTH % GK == 0, "whole requests");
+    constexpr size_t STAGED = WGK == 2 ? (size_t)BM * BN * 4 : 0;
+    static_assert(STAGED + 8 * GK * 16 * PITCH <= G::ring, "the ring's LDS");
+    unsigned char *const stage = smem + STAGED + wave * (GK * 16 * PITCH);
+    constexpr int AHEAD = !ADD ? 1 : J * MTH <= 16 * GK ? MTH / GK : 16 / J;      // groups of rows whose old values are requested ahead
+    uint4 old[ADD ? AHEAD * J : 1];
+    auto slot_row = [&](int j) { return (lane + 64 * j) / CH; };
+    auto slot_col = [&](int j) { return n0 + wn + (lane + 64 * j) % CH * 8; };
+    // destination row of slot j of the group that begins with row k of MTH, from the lanes that hold the rows'
+    auto slot_to = [&](int k, int j) {
+        const int r = slot_row(j);
+        const int one = __shfl(drow[k], r & 15, 64);
+        if constexpr (GK == 1) return one;
+        const int two = __shfl(drow[k + GK - 1], r & 15, 64);
+        return r < 16 ? one : two;
+    };
+    auto load_old = [&](int g) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p) old[k % AHEAD][p] = *reinterpret_cast<const uint4 *>(row + (ncol + 32 * p < a.N ? ncol + 32 * p : 0));
-        if constexpr (NT % 2) old1[k % AHEAD] = *reinterpret_cast<const uint2 *>(row + (ncol1 < a.N ? ncol1 : 0));
+        for (int j = 0; j < J; ++j) {
+            const int to = slot_to(g * GK, j), col = slot_col(j);
+            old[g % AHEAD * J + j] = *reinterpret_cast<const uint4 *>(a.C + (long)max(to, 0) * a.ld.c + (col < a.N ? col : 0));      // a row that is not stored reads row 0 and drops the value
+        }
     };
     auto load_epilogue = [&]() {
 #pragma unroll
@@ -323,7 +334,7 @@ gemm_i8_wide_kernel(GemmI8Args a, GemmTileRange tr)
     }
     if (!EARLY) load_epilogue();
 
-    // ---- epilogue, straight from the accumulators: lane (l16, quad) holds row 16*i + l16, columns 8*quad .. + 7 of every pair of tiles
+    // ---- epilogue: lane (l16, quad) holds row 16*i + l16, columns 8*quad .. + 7 of every pair of tiles
     i32x4 fin[MTH][NT];
     if constexpr (WGK == 2) {
         // the halves of K: either group sends the rows that the other one finishes, through the ring, whose last slab every wave had read at the last barrier
@@ -348,54 +359,128 @@ gemm_i8_wide_kernel(GemmI8Args a, GemmTileRange tr)
             for (int j = 0; j < NT; ++j) fin[k][j] = acc[k][j];
     }
 #pragma unroll
-    for (int k = 0; k < MTH; ++k) {
-        bf16 *row = a.C + (long)drow[k] * a.ld.c;
+    for (int g = 0; g < MTH / GK; ++g) {
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            float v[8];
+        for (int i = 0; i < GK; ++i) {
+            const int k = g * GK + i;
+            unsigned char *const at = stage + (16 * i + l16) * PITCH;
+            auto value = [&](int j, int e) { return gemm_i8_value<EPI>(fin[k][j][e], cs[j][e], rs[k], bv[j][e]); };
+            auto packed = [&](int j) { return make_uint2(pack_bf16x2(value(j, 0), value(j, 1)), pack_bf16x2(value(j, 2), value(j, 3))); };
+            // of a pair of tiles the first has columns 0 to 3 and the second 4 to 7 of chunk 4 * (pair) + quad; of an odd one two quads share a chunk
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = gemm_i8_value<EPI>(fin[k][2 * p + e / 4][e % 4], cs[2 * p + e / 4][e % 4], rs[k], bv[2 * p + e / 4][e % 4]);
-            if constexpr (ADD) {
-                float o[8];
-                unpack_bf16x8(old[k % AHEAD][p], o);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += o[e];
+            for (int j = 0; j < NT; ++j) {
+                const int four = j < 2 * NP ? 2 * (4 * (j / 2) + quad) + j % 2 : 8 * NP + quad;
+                if constexpr (ADD) *reinterpret_cast<f32x4 *>(at + 16 * four) = f32x4{ value(j, 0), value(j, 1), value(j, 2), value(j, 3) };
+                else if (j >= 2 * NP) *reinterpret_cast<uint2 *>(at + 8 * four) = packed(j);
+                else if (j % 2 == 0) {
+                    const uint2 lo = packed(j), hi = packed(j + 1 < NT ? j + 1 : j);
+                    *reinterpret_cast<uint4 *>(at + 8 * four) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+                }
             }
-            if (drow[k] >= 0 && ncol + 32 * p < a.N) *reinterpret_cast<uint4 *>(row + ncol + 32 * p) = pack_bf16x8(v);      // N % 8 == 0
         }
-        if constexpr (NT % 2) {
-            float v[4];
+        wave_lds_fence();
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = gemm_i8_value<EPI>(fin[k][NT - 1][e], cs[2 * NP][e], rs[k], bv[2 * NP][e]);
+        for (int j = 0; j < J; ++j) {
+            const int to = slot_to(g * GK, j), col = slot_col(j);
+            const unsigned char *const from = stage + slot_row(j) * PITCH + (lane + 64 * j) % CH * (ADD ? 32 : 16);
+            uint4 out;
             if constexpr (ADD) {
-                v[0] += __uint_as_float(old1[k % AHEAD].x << 16); v[1] += __uint_as_float(old1[k % AHEAD].x & 0xffff0000u);
-                v[2] += __uint_as_float(old1[k % AHEAD].y << 16); v[3] += __uint_as_float(old1[k % AHEAD].y & 0xffff0000u);
+                float v[8], o[8];
+                unpack_bf16x8(old[g % AHEAD * J + j], o);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const float *>(from)[e] + o[e];
+                out = pack_bf16x8(v);
+            } else {
+                out = *reinterpret_cast<const uint4 *>(from);
             }
-            if (drow[k] >= 0 && ncol1 < a.N) *reinterpret_cast<uint2 *>(row + ncol1) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            // (past the caches: what was there stays)
+            if (to >= 0 && col < a.N) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, out), reinterpret_cast<u32x4 *>(a.C + (long)to * a.ld.c + col));      // N % 8 == 0
         }
-        if constexpr (ADD) if (k + AHEAD < MTH) load_old(k + AHEAD);
+        wave_lds_fence();
+        if constexpr (ADD) if (g + AHEAD < MTH / GK) load_old(g + AHEAD);
     }
+}
+
+template <int BM, int BN, int WGK, int EPI>
+__global__ void __launch_bounds__(512, 1)
+gemm_i8_wide_kernel(GemmI8Args a, GemmTileRange tr)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int per_xcd = (tr.tile_count + 7) / 8, tl = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (tl >= tr.tile_count) return;
+    int m0, n0;
+    gemm_tile_origin(tr, tl, 0, 1, 1, BM, BN, m0, n0);
+    gemm_i8_tile<BM, BN, WGK, EPI>(a, m0, n0, smem);
+}
+
+// Several rounds of workgroups, of which the last would be a part: tiles from tr.tile_begin on are cut into SUB_M x SUB_N pieces.  Half of the pieces come first and half last: every CU has
+// as much to do, and CUs that began with a piece are out of step with the others, so that what some write at the end of a tile goes to memory under the products of the rest.
+template <int BM, int BN, int SUB_M, int SUB_N, int EPI>
+__global__ void __launch_bounds__(512, 1)
+gemm_i8_wide_cut_kernel(GemmI8Args a, GemmTileRange tr)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    constexpr int SUBS = SUB_M * SUB_N;
+    const int xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
+    const int whole = tr.tile_begin, pieces = (tr.tile_count - whole) * SUBS;
+    auto share = [](int n, int x) { return (int)((long)n * x / 8); };                     // of n tiles, XCD x takes [share(n, x), share(n, x + 1))
+    const int w0 = share(whole, xcd), ws = share(whole, xcd + 1) - w0, p0 = share(pieces, xcd), ps = share(pieces, xcd + 1) - p0, first = ps / 2;
+    int m0, n0;
+    if (i >= first && i < first + ws) {
+        gemm_tile_origin(tr, w0 + i - first, 0, 1, 1, BM, BN, m0, n0);
+        gemm_i8_tile<BM, BN, 1, EPI>(a, m0, n0, smem);
+        return;
+    }
+    const int p = i < first ? i : i - ws;
+    if (p >= ps) return;
+    gemm_tile_origin(tr, whole + (p0 + p) / SUBS, (p0 + p) % SUBS, SUB_M, SUB_N, BM / SUB_M, BN / SUB_N, m0, n0);
+    if (m0 >= a.M || n0 >= a.N) return;
+    gemm_i8_tile<BM / SUB_M, BN / SUB_N, 1, EPI>(a, m0, n0, smem);
+}
+
+template <class Kernel>
+int gemm_i8_launch_kernel(Kernel kern, int workgroups, size_t lds, const GemmI8Args &a, const GemmTileRange &tr, hipStream_t st)
+{
+    // more than 64 KiB of LDS per workgroup needs the per-kernel opt-in (idempotent, host-side only)
+    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return SSAM_EHIP;
+    hipLaunchKernelGGL(kern, dim3(workgroups), dim3(512), lds, st, a, tr);
+    SSAM_CHECK_LAUNCH();
+    return SSAM_OK;
 }
 
 template <int BM, int BN, int WGK, int EPI>
 int gemm_i8_launch_tile(const GemmI8Args &a, hipStream_t st)
 {
-    constexpr size_t lds = GemmWide<BM, BN, WGK>::lds_bytes;
-    auto kern = gemm_i8_wide_kernel<BM, BN, WGK, EPI>;
-    // more than 64 KiB of LDS per workgroup needs the per-kernel opt-in (idempotent, host-side only)
-    if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return SSAM_EHIP;
     GemmTileRange tr = { ssam_div_up(a.M, BM), ssam_div_up(a.N, BN), 0, 0 };
     tr.tile_count = tr.tiles_m * tr.tiles_n;
-    hipLaunchKernelGGL(kern, dim3(ssam_div_up(tr.tile_count, 8) * 8), dim3(512), lds, st, a, tr);
-    SSAM_CHECK_LAUNCH();
-    return SSAM_OK;
+    return gemm_i8_launch_kernel(gemm_i8_wide_kernel<BM, BN, WGK, EPI>, ssam_div_up(tr.tile_count, 8) * 8, GemmWide<BM, BN, WGK>::lds_bytes, a, tr, st);
+}
+
+// Tiles that are cut, of so many: those past whole rounds of 256; of whole rounds, and where the pieces of the others would be more than a round, `round / SUBS` tiles more or less.
+inline int gemm_i8_cut_tiles(int tiles, int subs)
+{
+    const int rem = tiles % 256;
+    return rem * subs <= 256 ? rem : 0;
+}
+
+template <int BM, int BN, int SUB_M, int SUB_N, int EPI>
+int gemm_i8_launch_cut(const GemmI8Args &a, hipStream_t st)
+{
+    constexpr size_t lds0 = GemmWide<BM, BN, 1>::lds_bytes, lds1 = GemmWide<BM / SUB_M, BN / SUB_N, 1>::lds_bytes;
+    GemmTileRange tr = { ssam_div_up(a.M, BM), ssam_div_up(a.N, BN), 0, 0 };
+    tr.tile_count = tr.tiles_m * tr.tiles_n;
+    const int cut = gemm_i8_cut_tiles(tr.tile_count, SUB_M * SUB_N);
+    tr.tile_begin = tr.tile_count - cut;
+    const int workgroups = 8 * (ssam_div_up(tr.tile_begin, 8) + ssam_div_up((long)cut * SUB_M * SUB_N, 8));
+    return gemm_i8_launch_kernel(gemm_i8_wide_cut_kernel<BM, BN, SUB_M, SUB_N, EPI>, workgroups, lds0 > lds1 ? lds0 : lds1, a, tr, st);
 }
 
 // Tiles, in the order of their index in the time model (gemm_i8.hip).
 #define GEMM_I8_TILES(X)                                                                                       \
     X(0, 64, 64, 2) X(1, 96, 64, 2) X(2, 96, 96, 2) X(3, 64, 128, 2) X(4, 128, 128, 1) X(5, 128, 192, 1)         \
     X(6, 192, 128, 1) X(7, 256, 128, 1) X(8, 192, 192, 1) X(9, 192, 256, 1) X(10, 256, 192, 1) X(11, 256, 256, 1)
-constexpr int GEMM_I8_COUNT = 12;
+#define GEMM_I8_CUT_TILES(X) X(12, 256, 256, 1, 2) X(13, 192, 256, 1, 2) X(14, 256, 192, 2, 1) X(15, 192, 192, 3, 1)
+constexpr int GEMM_I8_COUNT = 16;
 
 template <int EPI>
 int gemm_i8_launch(int tile, const GemmI8Args &a, hipStream_t st)
@@ -403,6 +488,9 @@ int gemm_i8_launch(int tile, const GemmI8Args &a, hipStream_t st)
     switch (tile) {
 #define X(id, bm, bn, wgk) case id: return gemm_i8_launch_tile<bm, bn, wgk, EPI>(a, st);
     GEMM_I8_TILES(X)
+#undef X
+#define X(id, bm, bn, sm, sn) case id: return gemm_i8_launch_cut<bm, bn, sm, sn, EPI>(a, st);
+    GEMM_I8_CUT_TILES(X)
 #undef X
     default: return SSAM_EINVAL;
     }

@@ -84,7 +84,7 @@ int launch_few(int mt, const GemmI8Args &a, hipStream_t st)
 
 // A launch of r rounds (one workgroup per CU at a time) takes t0 + r * (t_round + t_slab per slab, t_gelu and t_add behind those epilogues) + t_mb per megabyte of C.
 struct I8Tile { int bm, bn; double t0, t_round, t_slab, t_gelu, t_add, t_mb; };
-constexpr I8Tile i8_tiles[GEMM_I8_COUNT] = {
+constexpr I8Tile i8_tiles[12] = {
     { 64, 64, 3.7, 0, 0.16, 0.262, 0, 0.326 },
     { 96, 64, 0, 4.18, 0.207, 0.375, 0.03, 0.246 },
     { 96, 96, 0, 4.66, 0.251, 0.336, 0.504, 0.223 },
@@ -98,7 +98,7 @@ constexpr I8Tile i8_tiles[GEMM_I8_COUNT] = {
     { 256, 192, 0.964, 5, 0.838, 3.1, 0, 0.194 },
     { 256, 256, 1.7, 4.96, 1.09, 4.28, 0, 0.207 } };
 
-constexpr int I8_FEW = 16;                    // forms: tiles by their index, and 16 + 0, 1, 2: few rows, 16, 32 or 64 a workgroup
+constexpr int I8_FEW = 32;                    // forms: tiles by their index, and 32 + 0, 1, 2: few rows, 16, 32 or 64 a workgroup
 
 int pick_form(int M, int N, int K, int epilogue)
 {
@@ -106,7 +106,7 @@ int pick_form(int M, int N, int K, int epilogue)
     const int slabs = ssam_div_up(K, GEMM_I8_BK);
     int best = 0;
     double best_us = 1e30;
-    for (int i = 0; i < GEMM_I8_COUNT; ++i) {
+    for (int i = 0; i < 12; ++i) {
         const I8Tile &t = i8_tiles[i];
         const long rounds = ((long)ssam_div_up(M, t.bm) * ssam_div_up(N, t.bn) + 255) / 256;
         const double us = t.t0 + rounds * (t.t_round + t.t_slab * slabs + (epilogue == SSAM_EPI_BIAS_GELU ? t.t_gelu : epilogue == SSAM_EPI_BIAS_SCATTER_ADD ? t.t_add : 0.0))
