@@ -47,7 +47,7 @@ class BlockCfg(C.Structure):
 # Argument types of the calls that take plain numbers and addresses (p: pointer, i: int, l: long, f: float, z: size_t): building the ctypes objects in Python took
 # 1 to 3 us of a call of 10 to 20.
 _KINDS = {"p": C.c_void_p, "i": C.c_int, "l": C.c_long, "f": C.c_float, "z": C.c_size_t}
-_ARGUMENTS = {"ssam_quantize_rows": "ppplip", "ssam_linear_i8": "pippippp" + "iiiii" + "piiip", "ssam_invert_rows": "pipiiip",
+_ARGUMENTS = {"ssam_quantize_rows": "ppplip", "ssam_linear_i8": "pippippp" + "iiiii" + "piiip", "ssam_linear_i8_as": "pippippp" + "iiiii" + "piiiip", "ssam_linear_i8_form": "iiii", "ssam_invert_rows": "pipiiip",
               "ssam_residual_norm": "ppppipppifpppifp" + "iiiiip", "ssam_residual_norm_i8": "ppppipppifpppifpp" + "iiiiip",
               "ssam_residual_norm_backward": "pppipppifppif" + "pppp" + "ppppp" + "iiiiipzp"}
 

@@ -456,7 +456,7 @@ int gemm_i8_launch_tile(const GemmI8Args &a, hipStream_t st)
     return gemm_i8_launch_kernel(gemm_i8_wide_kernel<BM, BN, WGK, EPI>, ssam_div_up(tr.tile_count, 8) * 8, GemmWide<BM, BN, WGK>::lds_bytes, a, tr, st);
 }
 
-// Tiles that are cut, of so many: those past whole rounds of 256; of whole rounds, and where the pieces of the others would be more than a round, `round / SUBS` tiles more or less.
+// Tiles of so many that are cut: those past whole rounds of 256, unless their pieces are more than a round.
 inline int gemm_i8_cut_tiles(int tiles, int subs)
 {
     const int rem = tiles % 256;
@@ -479,8 +479,8 @@ int gemm_i8_launch_cut(const GemmI8Args &a, hipStream_t st)
 #define GEMM_I8_TILES(X)                                                                                       \
     X(0, 64, 64, 2) X(1, 96, 64, 2) X(2, 96, 96, 2) X(3, 64, 128, 2) X(4, 128, 128, 1) X(5, 128, 192, 1)         \
     X(6, 192, 128, 1) X(7, 256, 128, 1) X(8, 192, 192, 1) X(9, 192, 256, 1) X(10, 256, 192, 1) X(11, 256, 256, 1)
-#define GEMM_I8_CUT_TILES(X) X(12, 256, 256, 1, 2) X(13, 192, 256, 1, 2) X(14, 256, 192, 2, 1) X(15, 192, 192, 3, 1)
-constexpr int GEMM_I8_COUNT = 16;
+#define GEMM_I8_CUT_TILES(X) X(12, 256, 256, 1, 2) X(13, 192, 256, 1, 2) X(14, 256, 192, 2, 1)
+constexpr int GEMM_I8_TILE_COUNT = 12, GEMM_I8_COUNT = 15;
 
 template <int EPI>
 int gemm_i8_launch(int tile, const GemmI8Args &a, hipStream_t st)

@@ -6,6 +6,7 @@ import torch
 import residual_reference as R
 from helpers import announce
 from paper_2605_17633_amd import binding as B
+from test_linear_i8_forms import CASES, FORMS
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -108,6 +109,54 @@ def test_linear(M, N, K):
         got = B.ssam_linear_i8(*d, old.to(DEV), epilogue=epi, row_map=rows.to(DEV), rows_per_batch=per, map_batch_stride=per, dst_rows_per_batch=tokens)
         assert torch.equal(got.cpu()[~new], old[~new])
         _check(got.cpu()[new], ref[new], off[new], "mapped")
+
+
+def _forced(form, epi, A, sa, W, sw, bias, C, rows):
+    """A call with its form forced (None: its own), from tensors of the device; rows: the map of the epilogues that have one."""
+    (M, K), N = A.shape, W.shape[0]
+    args = (A.data_ptr(), K, sa.data_ptr(), W.data_ptr(), K, sw.data_ptr(), bias.data_ptr(), C.data_ptr(), N, M, N, K, epi, rows.data_ptr(), M, M, len(C))
+    stream = torch.cuda.current_stream().cuda_stream
+    rc = B.lib().ssam_linear_i8(*args, stream) if form is None else B.lib().ssam_linear_i8_as(*args, form, stream)
+    assert rc == B.OK
+
+
+def _forms_agree(M, N, K, epi, forms, against=32):
+    gen = torch.Generator(device=DEV).manual_seed(M + N + K)
+    codes = lambda *s: torch.randint(-128, 128, s, generator=gen, device=DEV, dtype=torch.int8)  # noqa: E731
+    f = lambda n: torch.rand(n, generator=gen, device=DEV) * 0.02 + 0.001  # noqa: E731
+    t = codes(M, K), f(M), codes(N, K), f(N) / K ** 0.5, torch.randn(N, generator=gen, device=DEV)
+    mapped = epi in (B.EPI_BIAS_SCATTER, B.EPI_BIAS_SCATTER_ADD)
+    rows = torch.randperm(M + 2, generator=gen, device=DEV)[:M].to(torch.int32)
+    rows[torch.rand(M, generator=gen, device=DEV) < 0.1] = -1
+    old = torch.randn(M + 2 if mapped else M, N, generator=gen, device=DEV).to(BF)
+    want = old.clone()
+    _forced(against, epi, *t, want, rows)
+    for form in forms:
+        got = old.clone()
+        _forced(form, epi, *t, got, rows)
+        assert torch.equal(got, want), (form, M, N, K, epi)
+    return t, want
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_forms_in_their_place(case):
+    """The kernel that a call takes by itself: the bits of the one for few rows (sums are exact, and the rest is done alike)."""
+    form, epi, M, N, K = case
+    announce("linear_i8 form", *case)
+    assert B.lib().ssam_linear_i8_form(M, N, K, epi) == form
+    (A, sa, W, sw, bias), want = _forms_agree(M, N, K, epi, [None])
+    if epi == B.EPI_BIAS:
+        v = (A.double() @ W.double().t()) * sw.double() * sa.double()[:, None]
+        err = R.U * (3 * v.abs() + (v + bias.double()).abs()) * (1 + 4 * R.U)
+        _check(want, (v + bias.double()).cpu(), err.cpu(), "few rows")
+
+
+@pytest.mark.parametrize("epi", range(4))
+@pytest.mark.parametrize("M,N,K", [(1, 8, 16), (70, 72, 128), (257, 264, 144), (300, 520, 272), (513, 200, 400), (129, 776, 656), (390, 392, 784), (700, 1032, 1168), (1100, 1000, 48)])
+def test_forms_outside_their_place(M, N, K, epi):
+    """Every kernel on sizes that are no multiple of its tile, and on fewer slabs of K than its ring holds."""
+    announce("linear_i8 forms", M, N, K, epi)
+    _forms_agree(M, N, K, epi, [f for f in FORMS if f != 32])
 
 
 def test_sums_are_exact():
