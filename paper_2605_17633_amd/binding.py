@@ -715,11 +715,21 @@ def _address(t, dtype, here, name):
     """Address of a dense tensor on the current device, None for None (what _dev and _one_device check, in fewer steps)."""
     if t is None:
         return None
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_contiguous() and t.get_device() == here:
-        return t.data_ptr()
+    try:
+        if t.dtype is dtype and t.is_contiguous() and t.get_device() == here:
+            return t.data_ptr()
+    except AttributeError:
+        pass
     _dev(t, dtype, name)
     _one_device(**{name: t})
     raise TypeError(f"{name}: expected a contiguous device tensor of {dtype}")
+
+
+def _vector(t, n, here, name):
+    """Address of fp32 [n]."""
+    if t is not None and t.shape != (n,):
+        _shape(t, (n,), name)
+    return _address(t, _FP32, here, name)
 
 
 def _here(t, name):
@@ -731,10 +741,13 @@ def _here(t, name):
 
 def _address_rows(t, dtype, here, name):
     """Address and row stride of a 2-D tensor whose rows are contiguous (a column slice is fine)."""
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 2 and t.get_device() == here:
-        stride, step = t.stride()
-        if step == 1:
-            return t.data_ptr(), stride
+    try:
+        if t.dtype is dtype and t.get_device() == here:
+            stride, step = t.stride()
+            if step == 1:
+                return t.data_ptr(), stride
+    except (AttributeError, ValueError):
+        pass
     _rows(t, dtype, name)
     _one_device(**{name: t})
     raise TypeError(f"{name}: expected a 2-D device tensor of {dtype} with contiguous rows")
@@ -743,43 +756,60 @@ def _address_rows(t, dtype, here, name):
 def ssam_quantize_rows(x, codes=None, scales=None):
     """x [..., D] bf16 (tokens, or a weight [out, in]) -> (codes [..., D] int8, scales [...] fp32, one for each row)."""
     here, shape = _here(x, "x"), x.shape
-    px, D = _address(x, _BF16, here, "x"), shape[-1]
+    px, rows, D = _address(x, _BF16, here, "x"), shape[:-1], shape[-1]
     if codes is None:
         codes = torch.empty_like(x, dtype=_INT8)
+        pc = codes.data_ptr()
+    else:
+        _shape(codes, shape, "codes")
+        pc = _address(codes, _INT8, here, "codes")
     if scales is None:
-        scales = x.new_empty(shape[:-1], dtype=_FP32)
-    _shape(codes, shape, "codes")
-    _shape(scales, shape[:-1], "scales")
-    _check("ssam_quantize_rows", lib().ssam_quantize_rows(px, _address(codes, _INT8, here, "codes"), _address(scales, _FP32, here, "scales"), x.numel() // D if D else 0, D, _stream()))
+        scales = x.new_empty(rows, dtype=_FP32)
+        ps = scales.data_ptr()
+    else:
+        _shape(scales, rows, "scales")
+        ps = _address(scales, _FP32, here, "scales")
+    rc = lib().ssam_quantize_rows(px, pc, ps, x.numel() // D if D else 0, D, _stream())
+    if rc:
+        _check("ssam_quantize_rows", rc)
     return codes, scales
 
 
 def ssam_linear_i8(A, a_scales, W, w_scales, bias, C_out=None, epilogue=EPI_BIAS, row_map=None, rows_per_batch=1, map_batch_stride=0, dst_rows_per_batch=1):
     """A [M,K], W [N,K] int8 with a_scales [M], w_scales [N], bias [N] fp32 -> C [M,N] bf16, or C_out updated through the row map (as for ssam_linear).
     A, W and C_out may be column slices of wider tensors."""
-    (M, K), N = A.shape, W.shape[0]
-    mapped = epilogue in (EPI_BIAS_SCATTER_ADD, EPI_BIAS_SCATTER)
-    _shape(W, (N, K), "W")
-    _shape(a_scales, (M,), "a_scales")
-    _shape(w_scales, (N,), "w_scales")
-    _shape(bias, (N,), "bias")
-    if mapped:
+    M, K = A.shape
+    N = W.shape[0]
+    if W.shape != (N, K):
+        _shape(W, (N, K), "W")
+    for name, t, n in (("a_scales", a_scales, M), ("w_scales", w_scales, N), ("bias", bias, N)):
+        if t.shape != (n,):
+            _shape(t, (n,), name)
+    pm = pc = None
+    if epilogue == EPI_BIAS_SCATTER_ADD or epilogue == EPI_BIAS_SCATTER:
         if C_out is None or row_map is None or rows_per_batch <= 0:
             raise ValueError("a mapped epilogue needs C_out, row_map and rows_per_batch")
-        batches = -(-M // rows_per_batch)
-        if row_map.numel() < max((batches - 1) * map_batch_stride + M - (batches - 1) * rows_per_batch, (batches - 2) * map_batch_stride + rows_per_batch if batches > 1 else 0):
+        last = -(-M // rows_per_batch) - 1               # the last image, which may have fewer rows
+        if row_map.numel() < max(last * map_batch_stride + M - last * rows_per_batch, (last - 1) * map_batch_stride + rows_per_batch if last else 0):
             raise ValueError(f"row_map: {row_map.numel()} entries do not cover {M} rows")
-        if C_out.dim() != 2 or C_out.shape[1] != N or C_out.shape[0] < batches * dst_rows_per_batch:
-            raise ValueError(f"C: shape {tuple(C_out.shape)}, expected [{batches * dst_rows_per_batch}, {N}] or more rows")
-    elif C_out is None:
-        C_out = A.new_empty((M, N), dtype=_BF16)
-    else:
+        if C_out.dim() != 2 or C_out.shape[1] != N or C_out.shape[0] < (last + 1) * dst_rows_per_batch:
+            raise ValueError(f"C: shape {tuple(C_out.shape)}, expected [{(last + 1) * dst_rows_per_batch}, {N}] or more rows")
+    elif C_out is not None:
         _shape(C_out, (M, N), "C")
     here = _here(A, "A")
-    (pa, lda), (pw, ldw), (pc, ldc) = _address_rows(A, _INT8, here, "A"), _address_rows(W, _INT8, here, "W"), _address_rows(C_out, _BF16, here, "C")
-    _check("ssam_linear_i8", lib().ssam_linear_i8(
-        pa, lda, _address(a_scales, _FP32, here, "a_scales"), pw, ldw, _address(w_scales, _FP32, here, "w_scales"), _address(bias, _FP32, here, "bias"), pc, ldc, M, N, K,
-        epilogue, _address(row_map, _INT32, here, "row_map"), rows_per_batch, map_batch_stride, dst_rows_per_batch, _stream()))
+    pa, lda = _address_rows(A, _INT8, here, "A")
+    pw, ldw = _address_rows(W, _INT8, here, "W")
+    psa, psw, pb = _address(a_scales, _FP32, here, "a_scales"), _address(w_scales, _FP32, here, "w_scales"), _address(bias, _FP32, here, "bias")
+    if row_map is not None:
+        pm = _address(row_map, _INT32, here, "row_map")
+    if C_out is None:
+        C_out = A.new_empty((M, N), dtype=_BF16)
+        pc, ldc = C_out.data_ptr(), N
+    else:
+        pc, ldc = _address_rows(C_out, _BF16, here, "C")
+    rc = lib().ssam_linear_i8(pa, lda, psa, pw, ldw, psw, pb, pc, ldc, M, N, K, epilogue, pm, rows_per_batch, map_batch_stride, dst_rows_per_batch, _stream())
+    if rc:
+        _check("ssam_linear_i8", rc)
     return C_out
 
 
@@ -800,8 +830,10 @@ def _token_map(t, B, N, here, name):
     """Address and batch stride of a map of tokens: [N] or [1,N] for all images, [B,N] for each."""
     if t is None:
         return None, 0
-    each = t.dim() == 2 and B > 1 and t.shape[0] == B
-    _shape(t, (B, N) if each else (N,) if t.dim() == 1 else (1, N), name)
+    shape = t.shape
+    each = B > 1 and shape == (B, N)
+    if not each and shape != (N,) and shape != (1, N):
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected {(N,)} or {(B, N)}")
     return _address(t, _INT32, here, name), N if each else 0
 
 
@@ -809,19 +841,23 @@ def _norm(pair, D, here, name):
     if pair is None:
         return None, None
     gain, shift = pair
-    _shape(gain, (D,), name)
-    _shape(shift, (D,), name)
-    return _address(gain, _FP32, here, name), _address(shift, _FP32, here, name)
+    return _vector(gain, D, here, name), _vector(shift, D, here, name)
 
 
 def _step_arguments(x, o, src, post, gate, dst, pre):
     """What the calls of a step share -> device, sizes, (o, src, its stride, post gain and shift, gate, its stride), (pre gain, shift), (dst, its stride)"""
     here, (B, N, D) = _here(x, "x"), x.shape
-    No = 0 if o is None else o.shape[1]
-    _shape(o, (B, No, D), "o")
-    each = gate is not None and gate.dim() == 2
-    _shape(gate, (B, D) if each else (D,), "gate")
-    branch = (_address(o, _BF16, here, "o"), *_token_map(src, B, N, here, "src"), *_norm(post, D, here, "post"), _address(gate, _FP32, here, "gate"), D if each else 0)
+    po, No, pg, each = None, 0, None, 0
+    if o is not None:
+        No = o.shape[1]
+        if o.shape != (B, No, D):
+            _shape(o, (B, No, D), "o")
+        po = _address(o, _BF16, here, "o")
+    if gate is not None:
+        each = D if gate.dim() == 2 else 0
+        _shape(gate, (B, D) if each else (D,), "gate")
+        pg = _address(gate, _FP32, here, "gate")
+    branch = (po, *_token_map(src, B, N, here, "src"), *_norm(post, D, here, "post"), pg, each)
     return here, B, N, No, D, branch, _norm(pre, D, here, "pre"), _token_map(dst, B, N, here, "dst")
 
 
@@ -891,16 +927,20 @@ def ssam_residual_norm_backward(x_out, o=None, src=None, post=None, gate=None, a
     dgate = dpost = dpre = None
     grads = (None, None, None, None)
     if weight_grads and not (gate is None and post is None and pre is None):
-        dgate = None if gate is None else torch.empty_like(gate)
-        grads = x_out.new_empty((4, D), dtype=_FP32).unbind(0)
-        dpost, dpre = grads[:2] if post else None, grads[2:] if pre else None
+        flat = gate is not None and gate.dim() == 1
+        grads = x_out.new_empty((4 + flat, D), dtype=_FP32).unbind(0)                     # one allocation for what is returned
+        dgate = grads[4] if flat else None if gate is None else torch.empty_like(gate)
+        dpost, dpre = grads[:2] if post else None, grads[2:4] if pre else None
         if workspace is None:
             workspace = x_out.new_empty(lib().ssam_residual_norm_backward_workspace_bytes(B, N, D, B if branch[-1] else 1), dtype=_U8)
-    dpost_g, dpost_b = (grads[0].data_ptr(), grads[1].data_ptr()) if dpost else (None, None)
-    dpre_g, dpre_b = (grads[2].data_ptr(), grads[3].data_ptr()) if dpre else (None, None)
+    at = [None, None, None, None]
+    if dpost:
+        at[:2] = grads[0].data_ptr(), grads[1].data_ptr()
+    if dpre:
+        at[2:] = grads[2].data_ptr(), grads[3].data_ptr()
     _check("ssam_residual_norm_backward", lib().ssam_residual_norm_backward(
         px, *branch, alpha, norm[0], *to, eps, _address(dy, _BF16, here, "dy"), _address(dx_out, _BF16, here, "dx_out"), _address(dx, _BF16, here, "dx"),
-        _address(do, _BF16, here, "do"), None if dgate is None else dgate.data_ptr(), dpost_g, dpost_b, dpre_g, dpre_b, B, N, No, Ny, D, _address(workspace, _U8, here, "workspace"),
+        _address(do, _BF16, here, "do"), None if dgate is None else dgate.data_ptr(), *at, B, N, No, Ny, D, _address(workspace, _U8, here, "workspace"),
         0 if workspace is None else workspace.numel(), _stream()))
     return dx, do, dgate, dpost, dpre
 

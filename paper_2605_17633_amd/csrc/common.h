@@ -140,24 +140,37 @@ __device__ __forceinline__ float gemm_quad_sum(float v)
 // wave_sum waits for the LDS (some 100 clocks; a row's two statistics and their gradients are 48 of them one after the other), one of these for the vector unit.
 template <int N> __device__ __forceinline__ uint32_t rotate16(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xf, 0xf, true); }
 template <int N> __device__ __forceinline__ float rotate16(float v) { return __uint_as_float(rotate16<N>(__float_as_uint(v))); }
+// LANES: 64, or 32 or 16: of every so many lanes by themselves.
+template <int LANES = 64>
 __device__ __forceinline__ float lanes_sum(float v)
 {
     v += rotate16<8>(v);
     v += rotate16<4>(v);
     v += rotate16<2>(v);
     v += rotate16<1>(v);
-    return gemm_quad_sum(v);
+    if constexpr (LANES == 64) return gemm_quad_sum(v);
+    if constexpr (LANES == 32) {
+        auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    }
+    return v;
 }
+template <int LANES = 64>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 {
     v = max(v, rotate16<8>(v));
     v = max(v, rotate16<4>(v));
     v = max(v, rotate16<2>(v));
     v = max(v, rotate16<1>(v));
-    auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    v = max(a[0], a[1]);
-    auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-    return max(b[0], b[1]);
+    if constexpr (LANES > 16) {
+        auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max(a[0], a[1]);
+    }
+    if constexpr (LANES > 32) {
+        auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max(b[0], b[1]);
+    }
+    return v;
 }
 
 // Sum over the 32 shares of a workgroup of 256 threads, thread = share * 8 + column: each column's is what share 0 gets.  In a fixed order.

@@ -10,19 +10,25 @@ namespace {
 constexpr int WAVES = 4;                      // of a workgroup
 constexpr long MOST_ROWS = 0x7fff0000L;       // row indices and what is added to them stay in 32 bits
 
-// The 16-byte chunks of a row that a lane has: lane, lane + 64, ...; one past the row re-reads the last one and is masked in the arithmetic.
-template <int MAXC>
+// Past the caches: of a step over 32768 x 1280 and its gradient, one behind the other, 173 -> 146 us, of a step between two contractions 3 % or nothing.  (Loads past the caches too: 169.)
+__device__ __forceinline__ void put16(uint4 *to, const uint4 &v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4 *>(to)); }
+__device__ __forceinline__ void put8(uint2 *to, const uint2 &v) { __builtin_nontemporal_store(__builtin_bit_cast(unsigned long, v), reinterpret_cast<unsigned long *>(to)); }
+
+// The 16-byte chunks of a row that a lane has: lane, lane + LANES, ...; one past the row re-reads the last one and is masked in the arithmetic.  LANES: of a row; rows of up to 256
+// features take 32 of a wave's, of up to 128 16 (65536 x 144 with a wave to a row 30.8 us, bound by arithmetic, now 18.5; its gradient 63, 40).
+template <int MAXC, int LANES>
 struct Chunks {
+    static_assert(LANES == 64 || MAXC == 1, "narrow rows");
     int at[MAXC];
     bool in[MAXC];
     float over_D;
     __device__ __forceinline__ Chunks(int chunks)
     {
-        const int lane = threadIdx.x & 63;
+        const int lane = threadIdx.x & (LANES - 1);
 #pragma unroll
         for (int i = 0; i < MAXC; ++i) {
-            in[i] = lane + 64 * i < chunks;
-            at[i] = min(lane + 64 * i, chunks - 1);
+            in[i] = lane + LANES * i < chunks;
+            at[i] = min(lane + LANES * i, chunks - 1);
         }
         over_D = 1.f / (float)(chunks * 8);
     }
@@ -35,7 +41,7 @@ struct Chunks {
     {
 #pragma unroll
         for (int i = 0; i < MAXC; ++i)
-            if (in[i]) row[at[i]] = pack_bf16x8(v[i]);
+            if (in[i]) put16(row + at[i], pack_bf16x8(v[i]));
     }
     __device__ __forceinline__ void unpack(const uint4 (&r)[MAXC], float (&v)[MAXC][8]) const
     {
@@ -56,12 +62,12 @@ struct Chunks {
         for (int i = 0; i < MAXC; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) s += in[i] ? v[i][e] : 0.f;
-        const float mean = lanes_sum(s) * over_D;
+        const float mean = lanes_sum<LANES>(s) * over_D;
 #pragma unroll
         for (int i = 0; i < MAXC; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) { v[i][e] = in[i] ? v[i][e] - mean : 0.f; q = fmaf(v[i][e], v[i][e], q); }
-        const float rstd = rsqrtf(lanes_sum(q) * over_D + eps);
+        const float rstd = rsqrtf(lanes_sum<LANES>(q) * over_D + eps);
 #pragma unroll
         for (int i = 0; i < MAXC; ++i)
 #pragma unroll
@@ -99,18 +105,26 @@ struct StepArgs {
 
 enum StepOut { STEP_NONE, STEP_BF16, STEP_8BIT };
 
-// One wave per token, its row and the branch's in registers.
-template <int MAXC, bool POST, StepOut OUT>
+// This wave, or part of one, of LANES lanes among all of the launch.
+template <int LANES>
+__device__ __forceinline__ int row_of_lanes()
+{
+    if constexpr (LANES == 64) return blockIdx.x * (blockDim.x / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    else return blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES;
+}
+
+// One wave, or part of one, per token, its row and the branch's in registers.
+template <int MAXC, int LANES, bool POST, StepOut OUT>
 __global__ void __launch_bounds__(256)
 residual_norm_kernel(StepArgs a)
 {
-    const int row = blockIdx.x * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = row_of_lanes<LANES>();
     if (row >= a.tokens) return;
     const int b = row / a.N, t = row - b * a.N;
     const int p = a.rows.branch(b, t), q = OUT == STEP_NONE ? -1 : a.rows.out(b, t);
     const bool writes = a.x_out && (p >= 0 || a.x_out != a.x);
     if (q < 0 && !writes) return;
-    const Chunks<MAXC> ch(a.chunks);
+    const Chunks<MAXC, LANES> ch(a.chunks);
     uint4 raw[MAXC];
     ch.load(a.x + (long)row * a.chunks, raw);
     float v[MAXC][8];
@@ -143,7 +157,7 @@ residual_norm_kernel(StepArgs a)
     if (writes) {
 #pragma unroll
         for (int i = 0; i < MAXC; ++i)
-            if (ch.in[i]) a.x_out[(long)row * a.chunks + ch.at[i]] = raw[i];
+            if (ch.in[i]) put16(a.x_out + (long)row * a.chunks + ch.at[i], raw[i]);
     }
     if constexpr (OUT != STEP_NONE) {
         if (q < 0) return;
@@ -167,31 +181,38 @@ residual_norm_kernel(StepArgs a)
             for (int i = 0; i < MAXC; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7fffffffu);
-            top = lanes_max(top);
+            top = lanes_max<LANES>(top);
             const bool finite = top < 0x7f800000u;
             const RowScale s = row_scale(finite ? __uint_as_float(top) : 0.f);
 #pragma unroll
             for (int i = 0; i < MAXC; ++i)
-                if (ch.in[i]) ((uint2 *)a.y)[to * a.chunks + ch.at[i]] = finite ? codes_of(v[i], s.inv) : make_uint2(0, 0);
-            if ((threadIdx.x & 63) == 0) a.scales[to] = finite ? s.scale : __uint_as_float(0x7fc00000u);
+                if (ch.in[i]) put8((uint2 *)a.y + to * a.chunks + ch.at[i], finite ? codes_of(v[i], s.inv) : make_uint2(0, 0));
+            if ((threadIdx.x & (LANES - 1)) == 0) a.scales[to] = finite ? s.scale : __uint_as_float(0x7fc00000u);
         }
     }
 }
 
-template <int MAXC>
+template <int MAXC, int LANES>
 int launch_step(const StepArgs &a, bool post, StepOut out, hipStream_t st)
 {
-    auto go = post ? (out == STEP_NONE ? residual_norm_kernel<MAXC, true, STEP_NONE> : out == STEP_BF16 ? residual_norm_kernel<MAXC, true, STEP_BF16> : residual_norm_kernel<MAXC, true, STEP_8BIT>)
-                   : (out == STEP_NONE ? residual_norm_kernel<MAXC, false, STEP_NONE> : out == STEP_BF16 ? residual_norm_kernel<MAXC, false, STEP_BF16> : residual_norm_kernel<MAXC, false, STEP_8BIT>);
-    hipLaunchKernelGGL(go, dim3(ssam_div_up(a.tokens, WAVES)), dim3(64 * WAVES), 0, st, a);
+    auto go = post ? (out == STEP_NONE ? residual_norm_kernel<MAXC, LANES, true, STEP_NONE> : out == STEP_BF16 ? residual_norm_kernel<MAXC, LANES, true, STEP_BF16> : residual_norm_kernel<MAXC, LANES, true, STEP_8BIT>)
+                   : (out == STEP_NONE ? residual_norm_kernel<MAXC, LANES, false, STEP_NONE> : out == STEP_BF16 ? residual_norm_kernel<MAXC, LANES, false, STEP_BF16> : residual_norm_kernel<MAXC, LANES, false, STEP_8BIT>);
+    hipLaunchKernelGGL(go, dim3(ssam_div_up(a.tokens, WAVES * 64 / LANES)), dim3(64 * WAVES), 0, st, a);
     SSAM_CHECK_LAUNCH();
     return SSAM_OK;
 }
 
-int launch_step(const StepArgs &a, bool post, StepOut out, hipStream_t st)
+// The kernel for rows of so many 16-byte chunks: call(MAXC, LANES)
+template <class Call>
+int by_width(int chunks, Call call)
 {
-    const int maxc = ssam_div_up(a.chunks, 64);
-    return maxc == 1 ? launch_step<1>(a, post, out, st) : maxc == 2 ? launch_step<2>(a, post, out, st) : maxc == 3 ? launch_step<3>(a, post, out, st) : launch_step<4>(a, post, out, st);
+    using std::integral_constant;
+    if (chunks <= 16) return call(integral_constant<int, 1>{}, integral_constant<int, 16>{});
+    if (chunks <= 32) return call(integral_constant<int, 1>{}, integral_constant<int, 32>{});
+    if (chunks <= 64) return call(integral_constant<int, 1>{}, integral_constant<int, 64>{});
+    if (chunks <= 128) return call(integral_constant<int, 2>{}, integral_constant<int, 64>{});
+    if (chunks <= 192) return call(integral_constant<int, 3>{}, integral_constant<int, 64>{});
+    return call(integral_constant<int, 4>{}, integral_constant<int, 64>{});
 }
 
 // ---------------------------------------------------------------- backward
@@ -229,7 +250,7 @@ constexpr size_t backward_lds(int maxc)
     return sizeof(float4) * 128 * maxc * (2 + (WEIGHTS ? back_waves(maxc) * vectors : 0));
 }
 
-template <int MAXC, bool POST, bool PRE, bool WEIGHTS>
+template <int MAXC, int LANES, bool POST, bool PRE, bool WEIGHTS>
 __global__ void __launch_bounds__(64 * back_waves(MAXC))
 residual_norm_backward_kernel(BackArgs a)
 {
@@ -237,12 +258,13 @@ residual_norm_backward_kernel(BackArgs a)
     extern __shared__ float4 lds4[];              // [2][2 MAXC][64] factors, then [wave][IN_LDS][2 MAXC][64]: halves of a lane's chunks, lanes side by side
     constexpr int VECTOR = 2 * MAXC * 64, BACK_WAVES = back_waves(MAXC);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const Chunks<MAXC> ch(a.chunks);
+    constexpr int PARTS = 64 / LANES;                          // rows of a wave
+    const Chunks<MAXC, LANES> ch(a.chunks);
     const float *gate = a.gate ? a.gate + (long)blockIdx.y * a.gate_stride : nullptr;
     float4 *const mine = lds4 + 2 * VECTOR + wave * (V::IN_LDS * VECTOR) + lane;
     // factors: of the second LayerNorm its gain, of the branch the gate times the first one's; zeros past the row
     for (int k = threadIdx.x; k < VECTOR; k += 64 * BACK_WAVES) {
-        const int c = (k & 63) + 64 * (k >> 7), quad = 2 * c + ((k >> 6) & 1);
+        const int c = (k & (LANES - 1)) + 64 * (k >> 7), quad = 2 * c + ((k >> 6) & 1);
         const bool in = c < a.chunks;
         float4 f = make_float4(0.f, 0.f, 0.f, 0.f), w = f;
         if (in && PRE) f = reinterpret_cast<const float4 *>(a.pre_g)[quad];
@@ -290,7 +312,7 @@ residual_norm_backward_kernel(BackArgs a)
     using std::integral_constant;
     constexpr float ONES[8] = { 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f };
 
-    const int stride = gridDim.x * BACK_WAVES;
+    const int stride = gridDim.x * BACK_WAVES * PARTS;
     struct Token { int row, p, q; long branch, out; };         // p, q < 0: no branch, no row of y
     auto token = [&](int r) {
         Token t = { -1, -1, -1, 0, 0 };
@@ -314,7 +336,7 @@ residual_norm_backward_kernel(BackArgs a)
         if (a.dx_out) ch.load(a.dx_out + at, rg);
         if (t.p >= 0) ch.load(a.o + t.branch, ro);
     };
-    int r = blockIdx.x * BACK_WAVES + wave;
+    int r = row_of_lanes<LANES>();
     Token now = token(r), next = token(r + stride);            // (tokens + 2 strides stay below 2^31)
     request(now);
     for (; r < a.tokens; r += stride) {
@@ -352,8 +374,8 @@ residual_norm_backward_kernel(BackArgs a)
                     s2 = fmaf(d[i][e], h[i][e], s2);
                 }
             }
-            s1 = lanes_sum(s1) * ch.over_D;
-            s2 = lanes_sum(s2) * ch.over_D;
+            s1 = lanes_sum<LANES>(s1) * ch.over_D;
+            s2 = lanes_sum<LANES>(s2) * ch.over_D;
 #pragma unroll
             for (int i = 0; i < MAXC; ++i)
 #pragma unroll
@@ -381,8 +403,8 @@ residual_norm_backward_kernel(BackArgs a)
                 }
             }
             if constexpr (POST) {
-                s1 = lanes_sum(s1) * ch.over_D;
-                s2 = lanes_sum(s2) * ch.over_D;
+                s1 = lanes_sum<LANES>(s1) * ch.over_D;
+                s2 = lanes_sum<LANES>(s2) * ch.over_D;
 #pragma unroll
                 for (int i = 0; i < MAXC; ++i)
 #pragma unroll
@@ -399,13 +421,16 @@ residual_norm_backward_kernel(BackArgs a)
         auto reduce = [&](int vector, int at, int pitch) {
             for (int k = threadIdx.x; k < VECTOR; k += 64 * BACK_WAVES) {
                 const int c = (k & 63) + 64 * (k >> 7);
-                float4 s = all[at + k];
+                if (c >= a.chunks || (k & 63) >= LANES) continue;
+                float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int w = 1; w < BACK_WAVES; ++w) {
-                    const float4 t = all[w * pitch + at + k];
-                    s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
-                }
-                if (c < a.chunks) out[(long)vector * 2 * a.chunks + 2 * c + ((k >> 6) & 1)] = s;
+                for (int w = 0; w < BACK_WAVES; ++w)
+#pragma unroll
+                    for (int g = 0; g < PARTS; ++g) {
+                        const float4 t = all[w * pitch + at + k + g * LANES];
+                        s.x += t.x; s.y += t.y; s.z += t.z; s.w += t.w;
+                    }
+                out[(long)vector * 2 * a.chunks + 2 * c + ((k >> 6) & 1)] = s;
             }
         };
         __syncthreads();
@@ -507,18 +532,19 @@ residual_image_sums_kernel(const float4 *__restrict__ images, int groups, Weight
 }
 
 // Workgroups that a group of tokens is dealt to: one to a CU over all groups.
-inline int backward_workgroups(long tokens, int groups, int maxc)
+inline int backward_workgroups(long tokens, int groups, int maxc, int lanes)
 {
-    const long most = ssam_div_up(256, groups), need = (tokens + back_waves(maxc) - 1) / back_waves(maxc);
+    const int rows = back_waves(maxc) * (64 / lanes);
+    const long most = ssam_div_up(256, groups), need = (tokens + rows - 1) / rows;
     return (int)(need < most ? need : most);
 }
 
-template <int MAXC, bool POST, bool PRE>
+template <int MAXC, int LANES, bool POST, bool PRE>
 int launch_backward(const BackArgs &a, const WeightGrads &w, bool weights, int groups, hipStream_t st)
 {
-    const int n = backward_workgroups(a.tokens, groups, MAXC);
+    const int n = backward_workgroups(a.tokens, groups, MAXC, LANES);
     const dim3 grid(n, groups);
-    auto kern = weights ? residual_norm_backward_kernel<MAXC, POST, PRE, true> : residual_norm_backward_kernel<MAXC, POST, PRE, false>;
+    auto kern = weights ? residual_norm_backward_kernel<MAXC, LANES, POST, PRE, true> : residual_norm_backward_kernel<MAXC, LANES, POST, PRE, false>;
     const size_t lds = weights ? backward_lds<POST, PRE, true>(MAXC) : backward_lds<POST, PRE, false>(MAXC);
     // more than 64 KiB of LDS per workgroup needs the per-kernel opt-in (idempotent, host-side only)
     if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) return SSAM_EHIP;
@@ -535,21 +561,21 @@ int launch_backward(const BackArgs &a, const WeightGrads &w, bool weights, int g
     return SSAM_OK;
 }
 
-template <int MAXC>
+template <int MAXC, int LANES>
 int launch_backward(const BackArgs &a, const WeightGrads &w, bool post, bool pre, bool weights, int groups, hipStream_t st)
 {
-    auto go = post ? (pre ? launch_backward<MAXC, true, true> : launch_backward<MAXC, true, false>) : (pre ? launch_backward<MAXC, false, true> : launch_backward<MAXC, false, false>);
+    auto go = post ? (pre ? launch_backward<MAXC, LANES, true, true> : launch_backward<MAXC, LANES, true, false>) : (pre ? launch_backward<MAXC, LANES, false, true> : launch_backward<MAXC, LANES, false, false>);
     return go(a, w, weights, groups, st);
 }
 
 // ---------------------------------------------------------------- rows in 8 bits
-// One wave per row: its largest magnitude, then its codes.  Rows of up to 64 * 8 * MAXC features stay in registers in between; MAXC = 0: longer ones are read twice.
-template <int MAXC>
+// One wave, or part of one, per row: its largest magnitude, then its codes.  Rows of up to 64 * 8 * MAXC features stay in registers in between; MAXC = 0: longer ones are read twice.
+template <int MAXC, int LANES>
 __global__ void __launch_bounds__(256)
 quantize_rows_kernel(const uint4 *__restrict__ x, uint2 *__restrict__ codes, float *__restrict__ scales, long rows, int chunks)
 {
-    const long row = (long)blockIdx.x * WAVES + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
+    const long row = (long)blockIdx.x * (WAVES * 64 / LANES) + threadIdx.x / LANES;
+    const int lane = threadIdx.x & (LANES - 1);
     if (row >= rows) return;
     x += row * chunks;
     codes += row * chunks;
@@ -557,26 +583,26 @@ quantize_rows_kernel(const uint4 *__restrict__ x, uint2 *__restrict__ codes, flo
     uint32_t top = 0;
     if constexpr (MAXC != 0) {
 #pragma unroll
-        for (int i = 0; i < MAXC; ++i) v[i] = x[min(lane + 64 * i, chunks - 1)];
+        for (int i = 0; i < MAXC; ++i) v[i] = x[min(lane + LANES * i, chunks - 1)];
 #pragma unroll
         for (int i = 0; i < MAXC; ++i) top = max_u16x2(top, top_of_bf16x8(v[i]));
     } else {
-        for (int c = lane; c < chunks; c += 64) top = max_u16x2(top, top_of_bf16x8(x[c]));
+        for (int c = lane; c < chunks; c += LANES) top = max_u16x2(top, top_of_bf16x8(x[c]));
     }
-    top = lanes_max(max(top >> 16, top & 0xffffu));
+    top = lanes_max<LANES>(max(top >> 16, top & 0xffffu));
     const bool finite = top < 0x7f80u;
     const RowScale s = row_scale(finite ? bf16_bits_to_float(top) : 0.f);
     auto put = [&](int c, const uint4 &r) {
         float f[8];
         unpack_bf16x8(r, f);
-        codes[c] = finite ? codes_of(f, s.inv) : make_uint2(0, 0);
+        put8(codes + c, finite ? codes_of(f, s.inv) : make_uint2(0, 0));
     };
     if constexpr (MAXC != 0) {
 #pragma unroll
         for (int i = 0; i < MAXC; ++i)
-            if (lane + 64 * i < chunks) put(lane + 64 * i, v[i]);
+            if (lane + LANES * i < chunks) put(lane + LANES * i, v[i]);
     } else {
-        for (int c = lane; c < chunks; c += 64) put(c, x[c]);
+        for (int c = lane; c < chunks; c += LANES) put(c, x[c]);
     }
     if (lane == 0) scales[row] = finite ? s.scale : __uint_as_float(0x7fc00000u);
 }
@@ -619,7 +645,7 @@ int step(const void *x, void *x_out, const void *o, const int32_t *src, int src_
     if (int rc = check_step(o, src, src_stride, post_g, post_b, gate, gate_stride, pre_g, dst, dst_stride, B, N, No, Ny, D); rc != SSAM_OK) return rc;
     const TokenRows rows = { src, dst, src_stride, dst_stride, o ? No : 0, pre_g ? Ny : 0 };
     const StepArgs a = { (const uint4 *)x, (uint4 *)x_out, (const uint4 *)o, rows, post_g, post_b, gate, pre_g, pre_b, gate_stride, alpha, eps, y, scales, B * N, N, D / 8 };
-    return launch_step(a, post_g != nullptr, out, (hipStream_t)stream);
+    return by_width(D / 8, [&](auto maxc, auto lanes) { return launch_step<decltype(maxc)::value, decltype(lanes)::value>(a, post_g != nullptr, out, (hipStream_t)stream); });
 }
 
 }  // namespace
@@ -639,10 +665,16 @@ extern "C" int ssam_quantize_rows(const void *x, void *codes, float *scales, lon
 {
     if (!x || !codes || !scales || rows <= 0 || D <= 0 || !ssam_aligned16(x) || !ssam_aligned16(codes) || !ssam_aligned16(scales)) return SSAM_EINVAL;
     if (D % 16 != 0 || D >= 131072 || rows > 4 * 0x7fffffffL) return SSAM_EUNSUPPORTED;
-    const int chunks = D / 8, maxc = ssam_div_up(chunks, 64);
-    auto go = maxc == 1 ? quantize_rows_kernel<1> : maxc == 2 ? quantize_rows_kernel<2> : maxc == 3 ? quantize_rows_kernel<3> : maxc == 4 ? quantize_rows_kernel<4>
-            : maxc <= 10 ? quantize_rows_kernel<10> : quantize_rows_kernel<0>;
-    hipLaunchKernelGGL(go, dim3((unsigned)((rows + WAVES - 1) / WAVES)), dim3(64 * WAVES), 0, (hipStream_t)stream, (const uint4 *)x, (uint2 *)codes, scales, rows, chunks);
+    const int chunks = D / 8;
+    auto go = [&](auto maxc, auto lanes) {
+        constexpr int MAXC = decltype(maxc)::value, LANES = decltype(lanes)::value, ROWS = WAVES * 64 / LANES;
+        hipLaunchKernelGGL((quantize_rows_kernel<MAXC, LANES>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(64 * WAVES), 0, (hipStream_t)stream,
+                           (const uint4 *)x, (uint2 *)codes, scales, rows, chunks);
+        return 0;
+    };
+    if (chunks <= 256) by_width(chunks, go);
+    else if (chunks <= 640) go(std::integral_constant<int, 10>{}, std::integral_constant<int, 64>{});
+    else go(std::integral_constant<int, 0>{}, std::integral_constant<int, 64>{});
     SSAM_CHECK_LAUNCH();
     return SSAM_OK;
 }
@@ -668,7 +700,7 @@ extern "C" int ssam_residual_norm_i8(const void *x, void *x_out, const void *o, 
 extern "C" size_t ssam_residual_norm_backward_workspace_bytes(int B, int N, int D, int gate_images)
 {
     if (B <= 0 || N <= 0 || D <= 0 || D > 2048 || (gate_images != 1 && gate_images != B)) return 0;
-    const int n = backward_workgroups(gate_images == 1 ? (long)B * N : N, gate_images, ssam_div_up(D, 512));
+    const int n = by_width(ssam_div_up(D, 8), [&](auto maxc, auto lanes) { return backward_workgroups(gate_images == 1 ? (long)B * N : N, gate_images, maxc, lanes); });
     return (size_t)gate_images * (n + (gate_images > 1)) * 4 * D * sizeof(float);
 }
 
@@ -693,7 +725,7 @@ extern "C" int ssam_residual_norm_backward(const void *x_out, const void *o, con
     const BackArgs a = { (const uint4 *)x_out, (const uint4 *)o, (const uint4 *)dy, (const uint4 *)dx_out, (uint4 *)dx, (uint4 *)d_o, rows, post_g, gate, pre_g,
                          gate_batch_stride, alpha, eps, (float *)workspace, groups > 1 ? N : B * N, N, D / 8 };
     const WeightGrads w = { post_g, post_b, gate, gate_batch_stride, dgate, dpost_g, dpost_b, dpre_g, dpre_b, D };
-    const int maxc = ssam_div_up(D / 8, 64);
-    auto go = maxc == 1 ? launch_backward<1> : maxc == 2 ? launch_backward<2> : maxc == 3 ? launch_backward<3> : launch_backward<4>;
-    return go(a, w, post_g != nullptr, pre_g != nullptr, weights, groups, (hipStream_t)stream);
+    return by_width(D / 8, [&](auto maxc, auto lanes) {
+        return launch_backward<decltype(maxc)::value, decltype(lanes)::value>(a, w, post_g != nullptr, pre_g != nullptr, weights, groups, (hipStream_t)stream);
+    });
 }

@@ -163,14 +163,14 @@ def test_gradients_without_what_comes_from_behind():
         assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("gate", ["features", "images"])
-def test_many_tokens_same_bits_and_workspace_bounds(gate):
+@pytest.mark.parametrize("gate,N,D", [("features", 1500, 1280), ("images", 1500, 1280), ("features", 6000, 64), ("images", 6000, 144), ("features", 1400, 2048)])
+def test_many_tokens_same_bits_and_workspace_bounds(gate, N, D):
     """More tokens than the waves of a launch; bytes around the workspace stay as they are; the same inputs give the same bits."""
-    case = (3, 1500, 1000, 700, 1280, True, gate, True, 0.9375, "each")
+    case = (3, N, 1000, 700, D, True, gate, True, 0.9375, "each")
     announce("residual_norm_backward", case)
     s = _inputs(case, 4)
     d, r = _dev(s), _double(s)
-    need = B.ssam_residual_norm_backward_workspace_bytes(3, 1500, 1280, 3 if gate == "images" else 1)
+    need = B.ssam_residual_norm_backward_workspace_bytes(3, N, D, 3 if gate == "images" else 1)
     room = torch.full((need + 512,), 77, dtype=torch.uint8, device=DEV)
     args = {k: d[k] for k in (*STEP, "dy", "dx_out")}
     runs = [B.ssam_residual_norm_backward(d["x"], **args, eps=EPS, workspace=room[256:256 + need]) for _ in range(2)]
