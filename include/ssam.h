@@ -242,7 +242,7 @@ int ssam_quantize_rows(const void *x, void *codes, float *scales, long rows, int
  * row).  A dev int8, rows of lda bytes; W dev int8 [N], rows of ldw bytes; a_scales dev fp32 [M]; w_scales, bias dev
  * fp32 [N]; C dev bf16, rows of ldc elements.  lda >= K, ldw >= K, multiples of 16; ldc >= N, a multiple of 8.  Any M;
  * N % 8 == 0, K % 16 == 0, K < 131072, lda and ldw up to 2^22, M and N below 2^31 - 65536, their
- * product below 2^40 and mapped rows of C below 2^31 (else SSAM_EUNSUPPORTED).  The result of
+ * product below 2^38 and mapped rows of C below 2^31 (else SSAM_EUNSUPPORTED).  The result of
  * a row does not depend on the other rows of the call.  No workspace, no atomics.  Codes are whole numbers: there is no gradient. */
 int ssam_linear_i8(const void *A, int lda, const float *a_scales, const void *W, int ldw, const float *w_scales,
                    const float *bias, void *C, int ldc, int M, int N, int K, int epilogue, const int32_t *row_map,

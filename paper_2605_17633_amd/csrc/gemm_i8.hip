@@ -10,6 +10,7 @@ int ssam_gemm_i8_scatter(int tile, const GemmI8Args &a, hipStream_t st);
 namespace {
 
 constexpr int I8_MOST_LD = 1 << 22, I8_MOST = 0x7fff0000;        // row and column indices and a tile more stay in 32 bits
+constexpr int I8_MOST_WORKGROUPS = (1 << 23) - 64;                 // of a launch, which has less than 2^32 threads
 
 // Few rows: 16 columns a workgroup, whose waves share K and add up in LDS.  Codes go from memory to the matrix unit's registers, past no barrier.
 template <int MT, int WAVES, int EPI>
@@ -81,7 +82,7 @@ int launch_few(int mt, const GemmI8Args &a, hipStream_t st)
     constexpr int WAVES = 8;
     auto kern = mt == 1 ? gemm_i8_few_kernel<1, WAVES, EPI> : gemm_i8_few_kernel<2, WAVES, EPI>;
     const long workgroups = (long)ssam_div_up(a.N, 16) * ssam_div_up(a.M, 16 * mt);
-    if (workgroups > 0x7fffffffL) return SSAM_EUNSUPPORTED;                 // forced (pick_form takes a tile)
+    if (workgroups > I8_MOST_WORKGROUPS) return SSAM_EUNSUPPORTED;          // forced (pick_form takes a tile)
     hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(64 * WAVES), 0, st, a);
     SSAM_CHECK_LAUNCH();
     return SSAM_OK;
@@ -118,13 +119,13 @@ int pick_form(int M, int N, int K, int epilogue)
 {
     const int slabs = ssam_div_up(K, GEMM_I8_BK);
     auto round = [&](const I8Tile &t) { return t.t_round + t.t_slab * slabs + (epilogue == SSAM_EPI_BIAS_GELU ? t.t_gelu : epilogue == SSAM_EPI_BIAS_SCATTER_ADD ? t.t_add : 0.0); };
-    int best = 0;
+    int best = 7;                             // 256x128: within the limit of workgroups at any size that is taken
     double best_us = 1e30;
     for (int form = 0; form < GEMM_I8_COUNT; ++form) {
         const I8Cut *cut = form < GEMM_I8_TILE_COUNT ? nullptr : &i8_cuts[form - GEMM_I8_TILE_COUNT];
         const I8Tile &t = i8_tiles[cut ? cut->tile : form];
         const long tiles = (long)ssam_div_up(M, t.bm) * ssam_div_up(N, t.bn);
-        if (cut && (tiles < 256 || gemm_i8_cut_tiles((int)tiles, cut->subs) == 0)) continue;
+        if (tiles > I8_MOST_WORKGROUPS || (cut && (tiles < 256 || gemm_i8_cut_tiles((int)tiles, cut->subs) == 0))) continue;
         const double us = t.t0 + (cut ? tiles / 256 * round(t) + round(i8_tiles[cut->piece]) : (tiles + 255) / 256 * round(t))
                         + (t.t_mb + (epilogue == SSAM_EPI_BIAS_SCATTER_ADD ? t.t_add_mb : 0.0)) * 2e-6 * M * N;
         if (us < best_us) { best_us = us; best = form; }
@@ -134,7 +135,7 @@ int pick_form(int M, int N, int K, int epilogue)
         const double w = (double)ssam_div_up(N, 16) * ssam_div_up(M, rows) / 256, k = K / 512.0, r = (M < rows ? M : rows) / 16.0;
         const I8Few &t = i8_few[i];
         const double us = t.t0 + k * (t.k + t.k_rows * r) + w * (t.w + k * (t.wk + t.wk_rows * r));
-        if (us < best_us && w * 256 < 0x7fffffff) { best_us = us; best = I8_FEW + i; }
+        if (us < best_us && w * 256 < I8_MOST_WORKGROUPS) { best_us = us; best = I8_FEW + i; }
     }
     return best;
 }
@@ -158,7 +159,7 @@ int linear_i8(const void *A, int lda, const float *a_scales, const void *W, int 
     const bool mapped = epilogue == SSAM_EPI_BIAS_SCATTER_ADD || epilogue == SSAM_EPI_BIAS_SCATTER;
     if (epilogue < 0 || epilogue > SSAM_EPI_BIAS_SCATTER) return SSAM_EINVAL;
     if (mapped && (!row_map || rows_per_batch <= 0 || map_batch_stride < 0 || dst_rows_per_batch <= 0)) return SSAM_EINVAL;
-    if (N % 8 != 0 || K % 16 != 0 || K >= 131072 || lda > I8_MOST_LD || ldw > I8_MOST_LD || (long)M * N >= 1L << 40 || M > I8_MOST || N > I8_MOST) return SSAM_EUNSUPPORTED;
+    if (N % 8 != 0 || K % 16 != 0 || K >= 131072 || lda > I8_MOST_LD || ldw > I8_MOST_LD || (long)M * N >= 1L << 38 || M > I8_MOST || N > I8_MOST) return SSAM_EUNSUPPORTED;
     if (mapped && (long)ssam_div_up(M, rows_per_batch) * dst_rows_per_batch > 0x7fffffffL) return SSAM_EUNSUPPORTED;
     const GemmI8Args a = { (const unsigned char *)A, (const unsigned char *)W, a_scales, w_scales, bias, (bf16 *)C, M, N, K, { lda, ldw, ldc },
                            { row_map, rows_per_batch, map_batch_stride, dst_rows_per_batch } };

@@ -9,6 +9,7 @@ namespace {
 
 constexpr int WAVES = 4;                      // of a workgroup
 constexpr long MOST_ROWS = 0x7fff0000L;       // row indices and what is added to them stay in 32 bits
+constexpr long MOST_WORKGROUPS = 1L << 22;    // of a launch, which has less than 2^32 threads
 
 // Past the caches: of a step over 32768 x 1280 and its gradient, one behind the other, 173 -> 146 us, of a step between two contractions 3 % or nothing.  (Loads past the caches too: 169.)
 __device__ __forceinline__ void put16(uint4 *to, const uint4 &v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4 *>(to)); }
@@ -100,7 +101,7 @@ struct StepArgs {
     float alpha, eps;
     void *y;
     float *scales;
-    int tokens, N, chunks;
+    int first, tokens, N, chunks;             // tokens from `first` on
 };
 
 enum StepOut { STEP_NONE, STEP_BF16, STEP_8BIT };
@@ -118,7 +119,7 @@ template <int MAXC, int LANES, bool POST, StepOut OUT>
 __global__ void __launch_bounds__(256)
 residual_norm_kernel(StepArgs a)
 {
-    const int row = row_of_lanes<LANES>();
+    const int row = a.first + row_of_lanes<LANES>();
     if (row >= a.tokens) return;
     const int b = row / a.N, t = row - b * a.N;
     const int p = a.rows.branch(b, t), q = OUT == STEP_NONE ? -1 : a.rows.out(b, t);
@@ -175,12 +176,12 @@ residual_norm_kernel(StepArgs a)
         if constexpr (OUT == STEP_BF16) {
             ch.store((uint4 *)a.y + to * a.chunks, v);
         } else {
-            // magnitudes order as their bits do, infinities and NaN highest (lanes past the row repeat its last values)
+            // magnitudes order as their bits do, infinities and NaN highest
             uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < MAXC; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7fffffffu);
+                for (int e = 0; e < 8; ++e) top = max(top, ch.in[i] ? __float_as_uint(v[i][e]) & 0x7fffffffu : 0u);
             top = lanes_max<LANES>(top);
             const bool finite = top < 0x7f800000u;
             const RowScale s = row_scale(finite ? __uint_as_float(top) : 0.f);
@@ -193,12 +194,17 @@ residual_norm_kernel(StepArgs a)
 }
 
 template <int MAXC, int LANES>
-int launch_step(const StepArgs &a, bool post, StepOut out, hipStream_t st)
+int launch_step(StepArgs a, bool post, StepOut out, hipStream_t st)
 {
     auto go = post ? (out == STEP_NONE ? residual_norm_kernel<MAXC, LANES, true, STEP_NONE> : out == STEP_BF16 ? residual_norm_kernel<MAXC, LANES, true, STEP_BF16> : residual_norm_kernel<MAXC, LANES, true, STEP_8BIT>)
                    : (out == STEP_NONE ? residual_norm_kernel<MAXC, LANES, false, STEP_NONE> : out == STEP_BF16 ? residual_norm_kernel<MAXC, LANES, false, STEP_BF16> : residual_norm_kernel<MAXC, LANES, false, STEP_8BIT>);
-    hipLaunchKernelGGL(go, dim3(ssam_div_up(a.tokens, WAVES * 64 / LANES)), dim3(64 * WAVES), 0, st, a);
-    SSAM_CHECK_LAUNCH();
+    constexpr int ROWS = WAVES * 64 / LANES;
+    for (long first = 0; first < a.tokens; first += MOST_WORKGROUPS * ROWS) {
+        a.first = (int)first;
+        const long left = ((long)a.tokens - first + ROWS - 1) / ROWS;
+        hipLaunchKernelGGL(go, dim3((unsigned)(left < MOST_WORKGROUPS ? left : MOST_WORKGROUPS)), dim3(64 * WAVES), 0, st, a);
+        SSAM_CHECK_LAUNCH();
+    }
     return SSAM_OK;
 }
 
@@ -644,7 +650,7 @@ int step(const void *x, void *x_out, const void *o, const int32_t *src, int src_
     if (o ? !x_out : x_out && x_out != x) return SSAM_EINVAL;
     if (int rc = check_step(o, src, src_stride, post_g, post_b, gate, gate_stride, pre_g, dst, dst_stride, B, N, No, Ny, D); rc != SSAM_OK) return rc;
     const TokenRows rows = { src, dst, src_stride, dst_stride, o ? No : 0, pre_g ? Ny : 0 };
-    const StepArgs a = { (const uint4 *)x, (uint4 *)x_out, (const uint4 *)o, rows, post_g, post_b, gate, pre_g, pre_b, gate_stride, alpha, eps, y, scales, B * N, N, D / 8 };
+    const StepArgs a = { (const uint4 *)x, (uint4 *)x_out, (const uint4 *)o, rows, post_g, post_b, gate, pre_g, pre_b, gate_stride, alpha, eps, y, scales, 0, B * N, N, D / 8 };
     return by_width(D / 8, [&](auto maxc, auto lanes) { return launch_step<decltype(maxc)::value, decltype(lanes)::value>(a, post_g != nullptr, out, (hipStream_t)stream); });
 }
 
@@ -664,19 +670,21 @@ extern "C" int ssam_invert_rows(const int32_t *idx, int idx_batch_stride, int32_
 extern "C" int ssam_quantize_rows(const void *x, void *codes, float *scales, long rows, int D, void *stream)
 {
     if (!x || !codes || !scales || rows <= 0 || D <= 0 || !ssam_aligned16(x) || !ssam_aligned16(codes) || !ssam_aligned16(scales)) return SSAM_EINVAL;
-    if (D % 16 != 0 || D >= 131072 || rows > 4 * 0x7fffffffL) return SSAM_EUNSUPPORTED;
+    if (D % 16 != 0 || D >= 131072 || rows >= 1L << 40) return SSAM_EUNSUPPORTED;
     const int chunks = D / 8;
-    auto go = [&](auto maxc, auto lanes) {
+    auto go = [&](auto maxc, auto lanes) -> int {
         constexpr int MAXC = decltype(maxc)::value, LANES = decltype(lanes)::value, ROWS = WAVES * 64 / LANES;
-        hipLaunchKernelGGL((quantize_rows_kernel<MAXC, LANES>), dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(64 * WAVES), 0, (hipStream_t)stream,
-                           (const uint4 *)x, (uint2 *)codes, scales, rows, chunks);
-        return 0;
+        for (long first = 0; first < rows; first += MOST_WORKGROUPS * ROWS) {
+            const long left = (rows - first + ROWS - 1) / ROWS;
+            hipLaunchKernelGGL((quantize_rows_kernel<MAXC, LANES>), dim3((unsigned)(left < MOST_WORKGROUPS ? left : MOST_WORKGROUPS)), dim3(64 * WAVES), 0, (hipStream_t)stream,
+                               (const uint4 *)x + first * chunks, (uint2 *)codes + first * chunks, scales + first, rows - first, chunks);
+            SSAM_CHECK_LAUNCH();
+        }
+        return SSAM_OK;
     };
-    if (chunks <= 256) by_width(chunks, go);
-    else if (chunks <= 640) go(std::integral_constant<int, 10>{}, std::integral_constant<int, 64>{});
-    else go(std::integral_constant<int, 0>{}, std::integral_constant<int, 64>{});
-    SSAM_CHECK_LAUNCH();
-    return SSAM_OK;
+    if (chunks <= 256) return by_width(chunks, go);
+    if (chunks <= 640) return go(std::integral_constant<int, 10>{}, std::integral_constant<int, 64>{});
+    return go(std::integral_constant<int, 0>{}, std::integral_constant<int, 64>{});
 }
 
 extern "C" int ssam_residual_norm(const void *x, void *x_out, const void *o, const int32_t *src, int src_batch_stride, const float *post_g, const float *post_b,

@@ -283,3 +283,28 @@ def test_a_block_in_8_bits():
     assert off(x1, r1) <= R.BF and off(x2, r2) <= 1e-2 and off(y, ref) <= 2e-2
     pad = (win < 0)
     assert bool((y[:, pad] == qkv[2].to(BF)).all())
+
+
+def test_tensors_past_32_bits():
+    """Codes and results of more than 2^31 elements, and more rows than a launch takes: the last rows are what they are alone."""
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    rows, D, tail = 1_100_000, 2048, 50
+    x = torch.ones(rows, D, dtype=BF, device=DEV)
+    x[-tail:] = torch.randn(tail, D, generator=gen, device=DEV).to(BF)
+    codes, scales = B.ssam_quantize_rows(x)
+    want, want_s = B.ssam_quantize_rows(x[-tail:].clone())
+    assert torch.equal(codes[-tail:], want) and torch.equal(scales[-tail:], want_s) and bool((codes[:-tail:1000] == 127).all())
+    del x
+    w, sw = B.ssam_quantize_rows(torch.randn(2056, D, generator=gen, device=DEV).to(BF))
+    bias = torch.randn(2056, generator=gen, device=DEV)
+    y = B.ssam_linear_i8(codes, scales, w, sw, bias)
+    assert y.numel() > 2 ** 31 and torch.equal(y[-tail:], B.ssam_linear_i8(want, want_s, w, sw, bias))
+    del y, codes
+    rows = (1 << 22) * 16 + 33
+    x = torch.zeros(rows, 16, dtype=BF, device=DEV)
+    x[-1] = torch.arange(16)
+    codes, scales = B.ssam_quantize_rows(x)
+    want = torch.from_numpy(R.quantised(np.arange(16.0)[None])[0][0]).to(DEV)
+    assert torch.equal(codes[-1], want) and not codes[:-1].any() and bool((scales[:-1] == 2.0 ** -126).all())
+    few = B.ssam_linear_i8(codes, scales, torch.ones(8, 16, dtype=torch.int8, device=DEV), torch.ones(8, device=DEV), torch.zeros(8, device=DEV))
+    assert not few[:-1].any() and bool((few[-1] == few[-1, 0]).all()) and abs(float(few[-1, 0]) - float(want.int().sum()) * 15 / 127) <= 2.0 ** -8 * 120.5

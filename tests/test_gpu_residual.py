@@ -286,3 +286,56 @@ def test_gradients_against_differences_of_the_call():
         curve = 0.0 if name == "pre" else h * h * float((wy.double().abs().sum()))
         announce("differences", name, ref, diff, noise, curve)
         assert abs(ref - diff) <= 5 * noise + curve, name
+
+
+def test_scales_are_of_the_row_alone():
+    """A shift of the last features that is larger than every value of the row: lanes past the row have no say in its scale."""
+    D = 1040
+    x = torch.randn(1, 3, D, generator=torch.Generator().manual_seed(0)) * 0.1
+    x[:, :, -8:] = -5.0
+    g, b = torch.ones(D), torch.zeros(D)
+    v = x.to(torch.bfloat16).double()
+    b[-8:] = -R.layer_norm(v, EPS)[0][0, 0, -8:].float()               # those features come out near 0, far below the others
+    _, codes, scales = B.ssam_residual_norm_i8(x.to(torch.bfloat16).to(DEV), pre=(g.to(DEV), b.to(DEV)), eps=EPS)
+    want = R.layer_norm(v, EPS)[0] + b.double()
+    top = want.abs().amax(2)
+    assert float(b.abs().max()) > 2 * float(top.max())
+    off = (R.layer_norm_error(v, EPS) + 2 * R.U * (want.abs() + b.double().abs())).amax(2) / 127 + 4 * R.U * top / 127
+    assert bool(((scales.cpu().double() - top / 127).abs() <= off).all()) and bool((codes.int().abs().amax(2) == 127).all())
+
+
+def test_tensors_past_32_bits():
+    """More than 2^31 elements: the last tokens are what the same tokens are alone."""
+    N, D, tail = 1_050_000, 2048, 40
+    x, o = (torch.empty(1, N, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    for t in (x, o):
+        t[:, :-tail] = 1.0
+        t[:, -tail:] = torch.randn(1, tail, D, generator=gen, device=DEV).to(torch.bfloat16)
+    norm = lambda: (1 + torch.randn(D, generator=gen, device=DEV) * 0.1, torch.randn(D, generator=gen, device=DEV) * 0.1)  # noqa: E731
+    post, pre, gate = norm(), norm(), torch.rand(D, generator=gen, device=DEV)
+    back = torch.arange(N - 1, -1, -1, dtype=torch.int32, device=DEV)                     # y in the other order: its first rows are the last tokens
+    x_out, y = B.ssam_residual_norm(x, o, None, post, gate, 0.9375, pre, back)
+    few = lambda t: t[:, -tail:].contiguous()  # noqa: E731
+    want_x, want_y = B.ssam_residual_norm(few(x), few(o), None, post, gate, 0.9375, pre)
+    assert torch.equal(few(x_out), want_x) and torch.equal(y[:, :tail].flip(1), want_y)
+    _, codes, scales = B.ssam_residual_norm_i8(x, o, None, post, gate, 0.9375, pre, x_out=x_out)
+    _, want_c, want_s = B.ssam_residual_norm_i8(few(x), few(o), None, post, gate, 0.9375, pre)
+    assert torch.equal(few(codes), want_c) and torch.equal(scales[:, -tail:], want_s)
+    del codes
+    dx, do, *_ = B.ssam_residual_norm_backward(x_out, o, None, post, gate, 0.9375, pre, None, dy=x, dx_out=o, do=y)
+    want = B.ssam_residual_norm_backward(few(x_out), few(o), None, post, gate, 0.9375, pre, None, dy=few(x), dx_out=few(o))
+    assert torch.equal(few(dx), want[0]) and torch.equal(few(do), want[1])
+
+
+def test_more_tokens_than_a_launch_takes():
+    N = (1 << 26) + (1 << 22) * 16 + 21
+    x = torch.ones(1, N, 8, dtype=torch.bfloat16, device=DEV)
+    x[0, -1] = torch.arange(8)
+    x[0, (1 << 22) * 16] = torch.arange(8)
+    _, y = B.ssam_residual_norm(x, pre=(torch.ones(8, device=DEV), torch.zeros(8, device=DEV)))
+    want = torch.nn.functional.layer_norm(torch.arange(8.0), (8,), eps=EPS).to(torch.bfloat16).to(DEV)
+    named = torch.tensor([N - 1, (1 << 22) * 16], device=DEV)
+    # (a step of bf16 is 2^-7 of the value; the row of ones has no deviation)
+    assert torch.allclose(y[0, named].float(), want.float().expand(2, -1), rtol=2 ** -7, atol=0)
+    assert int((y[0] != 0).any(1).sum()) == 2

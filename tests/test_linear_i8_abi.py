@@ -23,12 +23,13 @@ def test_linear_refuses(bad):
 
 
 @pytest.mark.parametrize("bad", [dict(N=28), dict(K=56), dict(K=131072, lda=131072, ldw=131072), dict(lda=(1 << 22) + 16), dict(ldw=(1 << 22) + 16),
-                                 dict(M=2 ** 31 - 1, N=1 << 15, ldc=1 << 15)])
+                                 dict(M=2 ** 31 - 65536, N=128, ldc=128),
+                                 dict(M=2 ** 31 - 65535), dict(M=1, N=2 ** 31 - 65528, ldc=2 ** 31 - 65528), dict(M=1 << 20, rows=1, stride=1, dst=1 << 11)])
 def test_linear_refuses_sizes(bad):
     assert linear(**bad) == B.EUNSUPPORTED
 
 
-@pytest.mark.parametrize("rows,D,want", [(0, 64, B.EINVAL), (-1, 64, B.EINVAL), (4, 0, B.EINVAL), (4, 56, B.EUNSUPPORTED), (1, 131072, B.EUNSUPPORTED), (1 << 34, 16, B.EUNSUPPORTED)])
+@pytest.mark.parametrize("rows,D,want", [(0, 64, B.EINVAL), (-1, 64, B.EINVAL), (4, 0, B.EINVAL), (4, 56, B.EUNSUPPORTED), (1, 131072, B.EUNSUPPORTED), (1 << 40, 16, B.EUNSUPPORTED)])
 def test_quantize_refuses_sizes(rows, D, want):
     assert B.lib().ssam_quantize_rows(P, P, P, C.c_long(rows), C.c_int(D), None) == want
 
