@@ -1,7 +1,18 @@
 // The contraction of 8-bit integers (gemm_i8.hip) for problems of more than a few rows: gemm_wide.h's schedule on the same bytes.  A slab of K is 128 bytes a row, two k-steps of the
-// 16x16x64 instruction, which reads the registers and takes the time of the bf16 one of 16x16x32: tiles, ring, swizzles and fragments are those of GemmWide.
+// 16x16x64 instruction, which reads the registers and takes the time (16 clocks) of the bf16 one of 16x16x32: tiles, ring, swizzles and fragments are those of GemmWide.
 // What differs: sums are whole numbers, so that halves of K add up exactly in any order; K is any multiple of 16 (a last slab's requests stay inside the row, and the fragments of one operand are
 // zeros from K on: whatever the other one holds there adds nothing); the epilogue scales by row and column.
+//
+// What bounds it.  Long K: 256x256 takes 1.4 to 1.6 us a slab (2.7 POP/s, at which the clock settles near 2 GHz): the matrix pipes 2050 of its 3000 clocks, and LDS as many (192 KB of fragments read
+// and 64 KB written by the requests, at 128 bytes a clock); neither is free while the other is not.  The block's K of 768 to 1280 are 6 to 10 slabs, and there a round's ends weigh as much: first slabs
+// from memory 2 us, and C, which is twice the bytes of A and W together.  So
+//   * results go through LDS and out in whole pieces of rows (64 to 192 bytes by lanes in order): straight from the accumulators 16 lanes write 16 bytes into each of 16 rows;
+//   * past the caches: C is as large as the L2s in every round, and pushed A and W out.  32768 x 3840 x 1280 as gemm_wide.h does it 192 us, with both 165 (skipping the stores: 140); one of the two alone 178.  What
+//     reads C next does not miss it: fc1, rows in 8 bits, fc2, LayerNorm of 13104 x 1280 x 5120 267 -> 237 us, of 1638 rows 52 -> 49;
+//   * tiles that are not a whole round are cut in pieces, half of them in front (192 -> 184 us before the stores were changed).
+// Measured (us; int8 library product, no scales nor bias, for comparison): 32768 x 3840 x 1280 165 (217), 13104 x 5120 x 1280 94, + GELU 114 (119), 13104 x 1280 x 5120 87 (99), + scatter-add 91, 4900 x 1280 x 1280 + scatter-add 16.1,
+// 4096 x 2304 x 768 12.8.  GELU costs 4.5 us a round of 256x256: its arithmetic, which nothing runs beside.  Not faster: results by whole lines of 128 bytes after an exchange between lanes (8 rows an
+// instruction, 30 % slower).
 #pragma once
 
 #include "gemm_wide.h"

@@ -114,7 +114,8 @@ __device__ __forceinline__ int row_of_lanes()
     else return blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES;
 }
 
-// One wave, or part of one, per token, its row and the branch's in registers.
+// One wave, or part of one, per token, its row and the branch's in registers; the norms' and the gate's vectors come from the caches.  Bound by HBM: 32768 x 1280 in the order of windows, 40 % of it
+// normed (285 MB) 61 us, 4.7 TB/s; 784 x 768 4.7 us; 16384 x 1024 with 40 % of the branch, in 8 bits (97 MB) 19 us.
 template <int MAXC, int LANES, bool POST, StepOut OUT>
 __global__ void __launch_bounds__(256)
 residual_norm_kernel(StepArgs a)
@@ -228,6 +229,8 @@ int by_width(int chunks, Call call)
 //   dgate = post_g sum(G h) + post_b sum(G) or sum(G o),  dpost_g = gate sum(G h),  dpost_b = gate sum(G);  with a gate of every image the first two are summed per image.
 // Waves walk the tokens and keep their share of the sums, two vectors in registers and the others in LDS (all four in registers leave one wave to a SIMD, under whose arithmetic
 // nothing is requested); the eight waves of a workgroup add theirs up, a second launch adds the workgroups' up, a third the images', all in a fixed order: no atomics, the same bits every time.
+// Bound by HBM: 32768 x 1280 (453 MB) 87 us, 5.2 TB/s, and 4 the sums; with sums over lanes through LDS 175, without those but all sums in registers and no token requested ahead 153.
+// 784 x 768: 7.6 and 3.5 us.
 struct BackArgs {
     const uint4 *x_out, *o, *dy, *dx_out;
     uint4 *dx, *d_o;
@@ -575,7 +578,7 @@ int launch_backward(const BackArgs &a, const WeightGrads &w, bool post, bool pre
 }
 
 // ---------------------------------------------------------------- rows in 8 bits
-// One wave, or part of one, per row: its largest magnitude, then its codes.  Rows of up to 64 * 8 * MAXC features stay in registers in between; MAXC = 0: longer ones are read twice.
+// One wave, or part of one, per row: its largest magnitude, then its codes.  Bound by HBM: 32768 x 1280 20 us (6.3 TB/s), 13104 x 5120 35 (5.7).  Rows of up to 64 * 8 * MAXC features stay in registers in between; MAXC = 0: longer ones are read twice.
 template <int MAXC, int LANES>
 __global__ void __launch_bounds__(256)
 quantize_rows_kernel(const uint4 *__restrict__ x, uint2 *__restrict__ codes, float *__restrict__ scales, long rows, int chunks)

@@ -339,3 +339,22 @@ def test_more_tokens_than_a_launch_takes():
     # (a step of bf16 is 2^-7 of the value; the row of ones has no deviation)
     assert torch.allclose(y[0, named].float(), want.float().expand(2, -1), rtol=2 ** -7, atol=0)
     assert int((y[0] != 0).any(1).sum()) == 2
+
+
+def test_rows_that_no_token_names_are_not_read():
+    """NaN in rows of the branch and of the gradient of y that no map names reaches nothing; outputs there stay as they were."""
+    case = (2, 40, 60, 50, 264, True, "images", True, 0.9375, "each")
+    d = _dev(_inputs(case, 10))
+    args = {k: d[k] for k in (*STEP, "dy", "dx_out")}
+    step = {k: d[k] for k in STEP}
+    want = (*B.ssam_residual_norm(d["x"], **step, eps=EPS, Ny=50), *B.ssam_residual_norm_backward(d["x"], **args, eps=EPS))
+    for name, which, rows in (("o", "src", 60), ("dy", "dst", 50)):
+        named = torch.zeros(2, rows + 1, dtype=torch.bool, device=DEV)
+        m = d[which].long()
+        named.scatter_(1, torch.where((m >= 0) & (m < rows), m, rows), True)
+        for t in (step, args):
+            if name in t:
+                t[name] = torch.where(named[:, :rows, None], t[name], float("nan"))
+    got = (*B.ssam_residual_norm(d["x"], **step, eps=EPS, Ny=50), *B.ssam_residual_norm_backward(d["x"], **args, eps=EPS))
+    for a, b in zip(got, want):
+        assert all(torch.equal(u, v) for u, v in zip(a, b)) if isinstance(a, tuple) else torch.equal(a, b)
