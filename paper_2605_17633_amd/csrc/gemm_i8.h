@@ -166,9 +166,9 @@ __device__ __forceinline__ void gemm_i8_tile(const GemmI8Args &a, int m0, int n0
     // accumulators 16 lanes write 16 rows, 16 bytes each.
     constexpr int CH = 2 * NT, GK = NT == 3 ? 2 : 1, J = GK * 16 * CH / 64, PITCH = CH * (ADD ? 32 : 16) + 16;
     static_assert(GK * 16 * CH % 64 == 0 && MTH % GK == 0, "whole requests");
-    constexpr size_t STAGED = WGK == 2 ? (size_t)BM * BN * 4 : 0;
-    static_assert(STAGED + 8 * GK * 16 * PITCH <= G::ring, "the ring's LDS");
-    unsigned char *const stage = smem + STAGED + wave * (GK * 16 * PITCH);
+    static_assert(8 * GK * 16 * PITCH <= G::ring, "the ring's LDS");
+    static_assert(WGK == 1 || 4 * 2 * MTH * NT * 64 * sizeof(i32x4) <= G::ring, "the halves are added in the ring's LDS");
+    unsigned char *const stage = smem + wave * (GK * 16 * PITCH);
     constexpr int AHEAD = !ADD ? 1 : J * MTH <= 16 * GK ? MTH / GK : 16 / J;      // groups of rows whose old values are requested ahead
     uint4 old[ADD ? AHEAD * J : 1];
     auto slot_row = [&](int j) { return (lane + 64 * j) / CH; };
@@ -363,6 +363,7 @@ __device__ __forceinline__ void gemm_i8_tile(const GemmI8Args &a, int m0, int n0
         for (int k = 0; k < MTH; ++k)
 #pragma unroll
             for (int j = 0; j < NT; ++j) fin[k][j] += x[(wk * MTH + k) * NT * 64 + j * 64];
+        LDS_BARRIER();                           // results are staged where other waves' halves lie
     } else {
 #pragma unroll
         for (int k = 0; k < MTH; ++k)
