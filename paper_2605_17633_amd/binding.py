@@ -87,10 +87,15 @@ def _check(name, rc):
 if hasattr(torch._C, "_cuda_getCurrentRawStream") and hasattr(torch._C, "_cuda_getDevice"):          # private names of torch
     _device = torch._C._cuda_getDevice
 
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+
     def _stream():
-        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+        return C.c_void_p(_raw_stream(_device()))
 else:
     _device = torch.cuda.current_device
+
+    def _raw_stream(device):
+        return torch.cuda.current_stream(device).cuda_stream
 
     def _stream():
         return C.c_void_p(torch.cuda.current_stream().cuda_stream)
@@ -725,13 +730,6 @@ def _address(t, dtype, here, name):
     raise TypeError(f"{name}: expected a contiguous device tensor of {dtype}")
 
 
-def _vector(t, n, here, name):
-    """Address of fp32 [n]."""
-    if t is not None and t.shape != (n,):
-        _shape(t, (n,), name)
-    return _address(t, _FP32, here, name)
-
-
 def _here(t, name):
     """The current device, for a call whose first tensor is t (without a GPU there is none to ask for)."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
@@ -769,7 +767,7 @@ def ssam_quantize_rows(x, codes=None, scales=None):
     else:
         _shape(scales, rows, "scales")
         ps = _address(scales, _FP32, here, "scales")
-    rc = lib().ssam_quantize_rows(px, pc, ps, x.numel() // D if D else 0, D, _stream())
+    rc = lib().ssam_quantize_rows(px, pc, ps, x.numel() // D if D else 0, D, _raw_stream(here))
     if rc:
         _check("ssam_quantize_rows", rc)
     return codes, scales
@@ -780,12 +778,10 @@ def ssam_linear_i8(A, a_scales, W, w_scales, bias, C_out=None, epilogue=EPI_BIAS
     A, W and C_out may be column slices of wider tensors."""
     M, K = A.shape
     N = W.shape[0]
-    if W.shape != (N, K):
-        _shape(W, (N, K), "W")
-    for name, t, n in (("a_scales", a_scales, M), ("w_scales", w_scales, N), ("bias", bias, N)):
-        if t.shape != (n,):
-            _shape(t, (n,), name)
-    pm = pc = None
+    if W.shape != (N, K) or a_scales.shape != (M,) or w_scales.shape != (N,) or bias.shape != (N,):
+        for name, t, want in (("W", W, (N, K)), ("a_scales", a_scales, (M,)), ("w_scales", w_scales, (N,)), ("bias", bias, (N,))):
+            _shape(t, want, name)
+    pm = None
     if epilogue == EPI_BIAS_SCATTER_ADD or epilogue == EPI_BIAS_SCATTER:
         if C_out is None or row_map is None or rows_per_batch <= 0:
             raise ValueError("a mapped epilogue needs C_out, row_map and rows_per_batch")
@@ -807,7 +803,7 @@ def ssam_linear_i8(A, a_scales, W, w_scales, bias, C_out=None, epilogue=EPI_BIAS
         pc, ldc = C_out.data_ptr(), N
     else:
         pc, ldc = _address_rows(C_out, _BF16, here, "C")
-    rc = lib().ssam_linear_i8(pa, lda, psa, pw, ldw, psw, pb, pc, ldc, M, N, K, epilogue, pm, rows_per_batch, map_batch_stride, dst_rows_per_batch, _stream())
+    rc = lib().ssam_linear_i8(pa, lda, psa, pw, ldw, psw, pb, pc, ldc, M, N, K, epilogue, pm, rows_per_batch, map_batch_stride, dst_rows_per_batch, _raw_stream(here))
     if rc:
         _check("ssam_linear_i8", rc)
     return C_out
@@ -822,7 +818,7 @@ def ssam_invert_rows(idx, N, inv=None):
         inv = idx.new_empty((*idx.shape[:-1], N))
     _shape(inv, (*idx.shape[:-1], N), "inv")
     B, Nout = (1, idx.shape[0]) if idx.dim() == 1 else idx.shape
-    _check("ssam_invert_rows", lib().ssam_invert_rows(pi, 0 if B == 1 else Nout, _address(inv, _INT32, here, "inv"), B, Nout, N, _stream()))
+    _check("ssam_invert_rows", lib().ssam_invert_rows(pi, 0 if B == 1 else Nout, _address(inv, _INT32, here, "inv"), B, Nout, N, _raw_stream(here)))
     return inv
 
 
@@ -841,7 +837,10 @@ def _norm(pair, D, here, name):
     if pair is None:
         return None, None
     gain, shift = pair
-    return _vector(gain, D, here, name), _vector(shift, D, here, name)
+    if gain.shape != (D,) or shift.shape != (D,):
+        _shape(gain, (D,), name)
+        _shape(shift, (D,), name)
+    return _address(gain, _FP32, here, name), _address(shift, _FP32, here, name)
 
 
 def _step_arguments(x, o, src, post, gate, dst, pre):
@@ -882,7 +881,7 @@ def ssam_residual_norm(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre
             y = x.new_empty((B, Ny, D)) if dst is None else x.new_zeros((B, Ny, D))
     _shape(y, (B, Ny, D), "y")
     _check("ssam_residual_norm", lib().ssam_residual_norm(
-        px, _address(x_out, _BF16, here, "x_out"), *branch, alpha, *norm, *to, eps, _address(y, _BF16, here, "y"), B, N, No, Ny, D, _stream()))
+        px, _address(x_out, _BF16, here, "x_out"), *branch, alpha, *norm, *to, eps, _address(y, _BF16, here, "y"), B, N, No, Ny, D, _raw_stream(here)))
     return x_out, y
 
 
@@ -899,7 +898,7 @@ def ssam_residual_norm_i8(x, o=None, src=None, post=None, gate=None, alpha=1.0, 
     _shape(scales, (B, Ny), "scales")
     _check("ssam_residual_norm_i8", lib().ssam_residual_norm_i8(
         px, _address(x_out, _BF16, here, "x_out"), *branch, alpha, *norm, *to, eps, _address(codes, _INT8, here, "codes"), _address(scales, _FP32, here, "scales"),
-        B, N, No, Ny, D, _stream()))
+        B, N, No, Ny, D, _raw_stream(here)))
     return x_out, codes, scales
 
 
@@ -941,7 +940,7 @@ def ssam_residual_norm_backward(x_out, o=None, src=None, post=None, gate=None, a
     _check("ssam_residual_norm_backward", lib().ssam_residual_norm_backward(
         px, *branch, alpha, norm[0], *to, eps, _address(dy, _BF16, here, "dy"), _address(dx_out, _BF16, here, "dx_out"), _address(dx, _BF16, here, "dx"),
         _address(do, _BF16, here, "do"), None if dgate is None else dgate.data_ptr(), *at, B, N, No, Ny, D, _address(workspace, _U8, here, "workspace"),
-        0 if workspace is None else workspace.numel(), _stream()))
+        0 if workspace is None else workspace.numel(), _raw_stream(here)))
     return dx, do, dgate, dpost, dpre
 
 
