@@ -12,7 +12,8 @@
 //   * tiles that are not a whole round are cut in pieces, half of them in front (192 -> 184 us before the stores were changed).
 // Measured (us; int8 library product, no scales nor bias, for comparison): 32768 x 3840 x 1280 165 (217), 13104 x 5120 x 1280 94, + GELU 114 (119), 13104 x 1280 x 5120 87 (99), + scatter-add 91, 4900 x 1280 x 1280 + scatter-add 16.1,
 // 4096 x 2304 x 768 12.8.  GELU costs 4.5 us a round of 256x256: its arithmetic, which nothing runs beside.  Not faster: results by whole lines of 128 bytes after an exchange between lanes (8 rows an
-// instruction, 30 % slower).
+// instruction, 30 % slower); two workgroups to a CU, of which one writes while the other multiplies: 128x128 in 128 registers 194 us of the first, 128x256 of four waves 187 (GELU as fast as now): they pull
+// twice and one and a half times the bytes of 256x256 from the L2.
 #pragma once
 
 #include "gemm_wide.h"
