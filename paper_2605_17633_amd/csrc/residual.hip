@@ -540,11 +540,13 @@ residual_image_sums_kernel(const float4 *__restrict__ images, int groups, Weight
     if (threadIdx.x < 8 && quad < quads) { put4(w.dpost_g, quad, s[0]); put4(w.dpost_b, quad, s[1]); }
 }
 
-// Workgroups that a group of tokens is dealt to: one to a CU over all groups.
+// Workgroups that a group of tokens is dealt to: no more than 256 over all groups, one to a CU, which holds one of rows above 512.  (Rounded up, 3, 5, 6 or 7 groups were 258 to 260, whose last few
+// ran alone for as long as the others: 7 x 4096 x 2048, a gate of every image, 236 us and now 150, 7 x 4096 x 1280 124 and 84, 3 x 4096 x 1280 60 and 45.)  Of rows up to 512 a CU holds two: above
+// 128 groups each has two workgroups (129 x 400 x 144 46 us, with one 55; 129 x 400 x 1024 168 with one, with two 201).
 inline int backward_workgroups(long tokens, int groups, int maxc, int lanes)
 {
     const int rows = back_waves(maxc) * (64 / lanes);
-    const long most = ssam_div_up(256, groups), need = (tokens + rows - 1) / rows;
+    const long most = groups >= 256 ? 1 : maxc == 1 && groups > 128 ? 2 : 256 / groups, need = (tokens + rows - 1) / rows;
     return (int)(need < most ? need : most);
 }
 
