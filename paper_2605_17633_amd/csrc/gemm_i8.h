@@ -476,16 +476,21 @@ inline int gemm_i8_cut_tiles(int tiles, int subs)
     return rem * subs <= 256 ? rem : 0;
 }
 
+// Workgroups of a launch of so many tiles: on every XCD its share of the whole ones and of the pieces.
+inline int gemm_i8_cut_workgroups(int tiles, int subs)
+{
+    const int cut = gemm_i8_cut_tiles(tiles, subs);
+    return 8 * (ssam_div_up(tiles - cut, 8) + ssam_div_up((long)cut * subs, 8));
+}
+
 template <int BM, int BN, int SUB_M, int SUB_N, int EPI>
 int gemm_i8_launch_cut(const GemmI8Args &a, hipStream_t st)
 {
     constexpr size_t lds0 = GemmWide<BM, BN, 1>::lds_bytes, lds1 = GemmWide<BM / SUB_M, BN / SUB_N, 1>::lds_bytes;
     GemmTileRange tr = { ssam_div_up(a.M, BM), ssam_div_up(a.N, BN), 0, 0 };
     tr.tile_count = tr.tiles_m * tr.tiles_n;
-    const int cut = gemm_i8_cut_tiles(tr.tile_count, SUB_M * SUB_N);
-    tr.tile_begin = tr.tile_count - cut;
-    const int workgroups = 8 * (ssam_div_up(tr.tile_begin, 8) + ssam_div_up((long)cut * SUB_M * SUB_N, 8));
-    return gemm_i8_launch_kernel(gemm_i8_wide_cut_kernel<BM, BN, SUB_M, SUB_N, EPI>, workgroups, lds0 > lds1 ? lds0 : lds1, a, tr, st);
+    tr.tile_begin = tr.tile_count - gemm_i8_cut_tiles(tr.tile_count, SUB_M * SUB_N);
+    return gemm_i8_launch_kernel(gemm_i8_wide_cut_kernel<BM, BN, SUB_M, SUB_N, EPI>, gemm_i8_cut_workgroups(tr.tile_count, SUB_M * SUB_N), lds0 > lds1 ? lds0 : lds1, a, tr, st);
 }
 
 // Tiles, in the order of their index in the time model (gemm_i8.hip).

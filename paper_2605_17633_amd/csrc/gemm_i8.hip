@@ -83,9 +83,7 @@ int launch_few(int mt, const GemmI8Args &a, hipStream_t st)
 {
     constexpr int WAVES = 8;
     auto kern = mt == 1 ? gemm_i8_few_kernel<1, WAVES, EPI> : gemm_i8_few_kernel<2, WAVES, EPI>;
-    const long workgroups = (long)ssam_div_up(a.N, 16) * ssam_div_up(a.M, 16 * mt);
-    if (workgroups > I8_MOST_WORKGROUPS) return SSAM_EUNSUPPORTED;          // forced (pick_form takes a tile)
-    hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(64 * WAVES), 0, st, a);
+    hipLaunchKernelGGL(kern, dim3(ssam_div_up(a.N, 16) * ssam_div_up(a.M, 16 * mt)), dim3(64 * WAVES), 0, st, a);
     SSAM_CHECK_LAUNCH();
     return SSAM_OK;
 }
@@ -117,17 +115,27 @@ constexpr I8Few i8_few[2] = { { 2.638, 0.243, 0.062, 0.057, 0.166, 0.219 }, { 2.
 
 constexpr int I8_FEW = 32;                    // forms: tiles by their index, and 32, 33: few rows, 16 or 32 a workgroup
 
+// Workgroups of a form's launch.
+long form_workgroups(int form, int M, int N)
+{
+    if (form >= I8_FEW) return (long)ssam_div_up(N, 16) * ssam_div_up(M, 16 << (form - I8_FEW));
+    const I8Cut *cut = form < GEMM_I8_TILE_COUNT ? nullptr : &i8_cuts[form - GEMM_I8_TILE_COUNT];
+    const I8Tile &t = i8_tiles[cut ? cut->tile : form];
+    const int tiles = ssam_div_up(M, t.bm) * ssam_div_up(N, t.bn);                          // (M * N < 2^38)
+    return cut ? gemm_i8_cut_workgroups(tiles, cut->subs) : ssam_div_up(tiles, 8) * 8;
+}
+
 int pick_form(int M, int N, int K, int epilogue)
 {
     const int slabs = ssam_div_up(K, GEMM_I8_BK);
     auto round = [&](const I8Tile &t) { return t.t_round + t.t_slab * slabs + (epilogue == SSAM_EPI_BIAS_GELU ? t.t_gelu : epilogue == SSAM_EPI_BIAS_SCATTER_ADD ? t.t_add : 0.0); };
-    int best = 7;                             // 256x128: within the limit of workgroups at any size that is taken
+    int best = GEMM_I8_TILE_COUNT - 1;        // 256x256: within the limit of workgroups at any size that is taken
     double best_us = 1e30;
     for (int form = 0; form < GEMM_I8_COUNT; ++form) {
         const I8Cut *cut = form < GEMM_I8_TILE_COUNT ? nullptr : &i8_cuts[form - GEMM_I8_TILE_COUNT];
         const I8Tile &t = i8_tiles[cut ? cut->tile : form];
         const long tiles = (long)ssam_div_up(M, t.bm) * ssam_div_up(N, t.bn);
-        if (tiles > I8_MOST_WORKGROUPS || (cut && (tiles < 256 || gemm_i8_cut_tiles((int)tiles, cut->subs) == 0))) continue;
+        if (form_workgroups(form, M, N) > I8_MOST_WORKGROUPS || (cut && (tiles < 256 || gemm_i8_cut_tiles((int)tiles, cut->subs) == 0))) continue;
         const double us = t.t0 + (cut ? tiles / 256 * round(t) + round(i8_tiles[cut->piece]) : (tiles + 255) / 256 * round(t))
                         + (t.t_mb + (epilogue == SSAM_EPI_BIAS_SCATTER_ADD ? t.t_add_mb : 0.0)) * 2e-6 * M * N;
         if (us < best_us) { best_us = us; best = form; }
@@ -137,7 +145,7 @@ int pick_form(int M, int N, int K, int epilogue)
         const double w = (double)ssam_div_up(N, 16) * ssam_div_up(M, rows) / 256, k = K / 512.0, r = (M < rows ? M : rows) / 16.0;
         const I8Few &t = i8_few[i];
         const double us = t.t0 + k * (t.k + t.k_rows * r) + w * (t.w + k * (t.wk + t.wk_rows * r));
-        if (us < best_us && w * 256 < I8_MOST_WORKGROUPS) { best_us = us; best = I8_FEW + i; }
+        if (us < best_us && form_workgroups(I8_FEW + i, M, N) <= I8_MOST_WORKGROUPS) { best_us = us; best = I8_FEW + i; }
     }
     return best;
 }
@@ -166,7 +174,7 @@ int linear_i8(const void *A, int lda, const float *a_scales, const void *W, int 
     const GemmI8Args a = { (const unsigned char *)A, (const unsigned char *)W, a_scales, w_scales, bias, (bf16 *)C, M, N, K, { lda, ldw, ldc },
                            { row_map, rows_per_batch, map_batch_stride, dst_rows_per_batch } };
     if (form < 0) form = pick_form(M, N, K, epilogue);
-    else if (form >= GEMM_I8_COUNT && (form < I8_FEW || form > I8_FEW + 1)) return SSAM_EUNSUPPORTED;
+    else if ((form >= GEMM_I8_COUNT && (form < I8_FEW || form > I8_FEW + 1)) || form_workgroups(form, M, N) > I8_MOST_WORKGROUPS) return SSAM_EUNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
     switch (epilogue) {
     case SSAM_EPI_BIAS: return launch<SSAM_EPI_BIAS>(form, a, st);
