@@ -714,6 +714,7 @@ def ssam_gelu_backward(codes, scales, da, dh=None, a=None, activation=True):
 
 # ------------------------------------------------------------------ 8-bit integers
 _BF16, _FP32, _INT32, _INT8, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
+_MOST_INT = 2 ** 31 - 1       # sizes and strides past it are refused here: ctypes would cut them to 32 bits, and the call would do a part of its work
 
 
 def _address(t, dtype, here, name):
@@ -755,6 +756,8 @@ def ssam_quantize_rows(x, codes=None, scales=None):
     """x [..., D] bf16 (tokens, or a weight [out, in]) -> (codes [..., D] int8, scales [...] fp32, one for each row)."""
     here, shape = _here(x, "x"), x.shape
     px, rows, D = _address(x, _BF16, here, "x"), shape[:-1], shape[-1]
+    if D > _MOST_INT:
+        raise SsamError("ssam_quantize_rows", EUNSUPPORTED)
     if codes is None:
         codes = torch.empty_like(x, dtype=_INT8)
         pc = codes.data_ptr()
@@ -785,6 +788,8 @@ def ssam_linear_i8(A, a_scales, W, w_scales, bias, C_out=None, epilogue=EPI_BIAS
     if epilogue == EPI_BIAS_SCATTER_ADD or epilogue == EPI_BIAS_SCATTER:
         if C_out is None or row_map is None or rows_per_batch <= 0:
             raise ValueError("a mapped epilogue needs C_out, row_map and rows_per_batch")
+        if max(rows_per_batch, map_batch_stride, dst_rows_per_batch) > _MOST_INT:
+            raise SsamError("ssam_linear_i8", EUNSUPPORTED)
         last = -(-M // rows_per_batch) - 1               # the last image, which may have fewer rows
         if row_map.numel() < max(last * map_batch_stride + M - last * rows_per_batch, (last - 1) * map_batch_stride + rows_per_batch if last else 0):
             raise ValueError(f"row_map: {row_map.numel()} entries do not cover {M} rows")
@@ -798,11 +803,12 @@ def ssam_linear_i8(A, a_scales, W, w_scales, bias, C_out=None, epilogue=EPI_BIAS
     psa, psw, pb = _address(a_scales, _FP32, here, "a_scales"), _address(w_scales, _FP32, here, "w_scales"), _address(bias, _FP32, here, "bias")
     if row_map is not None:
         pm = _address(row_map, _INT32, here, "row_map")
+    pc, ldc = (None, N) if C_out is None else _address_rows(C_out, _BF16, here, "C")
+    if max(M, N, K, lda, ldw, ldc) > _MOST_INT:
+        raise SsamError("ssam_linear_i8", EUNSUPPORTED)
     if C_out is None:
         C_out = A.new_empty(M, N, dtype=_BF16)
-        pc, ldc = C_out.data_ptr(), N
-    else:
-        pc, ldc = _address_rows(C_out, _BF16, here, "C")
+        pc = C_out.data_ptr()
     rc = lib().ssam_linear_i8(pa, lda, psa, pw, ldw, psw, pb, pc, ldc, M, N, K, epilogue, pm, rows_per_batch, map_batch_stride, dst_rows_per_batch, _raw_stream(here))
     if rc:
         _check("ssam_linear_i8", rc)
@@ -814,6 +820,8 @@ def ssam_invert_rows(idx, N, inv=None):
     """idx int32 [Nout] or [B,Nout]: the token of every slot, outside [0,N) none -> inv int32 [N] or [B,N]: the slot of every token, -1 none."""
     here = _here(idx, "idx")
     pi = _address(idx, _INT32, here, "idx")
+    if max(N, *idx.shape) > _MOST_INT:
+        raise SsamError("ssam_invert_rows", EUNSUPPORTED)
     if inv is None:
         inv = idx.new_empty((*idx.shape[:-1], N))
     _shape(inv, (*idx.shape[:-1], N), "inv")
@@ -843,10 +851,12 @@ def _norm(pair, D, here, name):
     return _address(gain, _FP32, here, name), _address(shift, _FP32, here, name)
 
 
-def _step_arguments(x, o, src, post, gate, dst, pre):
-    """What the calls of a step share -> device, sizes, (o, src, its stride, post gain and shift, gate, its stride), (pre gain, shift), (dst, its stride)"""
+def _step_arguments(name, x, o, src, post, gate, dst, pre, Ny):
+    """What the calls of a step share (Ny None: as many rows of y as tokens)
+    -> device, sizes, (o, src, its stride, post gain and shift, gate, its stride), (pre gain, shift), (dst, its stride)"""
     here, (B, N, D) = _here(x, "x"), x.shape
     po, No, pg, each = None, 0, None, 0
+    Ny = N if Ny is None else Ny
     if o is not None:
         No = o.shape[1]
         if o.shape != (B, No, D):
@@ -856,8 +866,10 @@ def _step_arguments(x, o, src, post, gate, dst, pre):
         each = D if gate.dim() == 2 else 0
         _shape(gate, (B, D) if each else (D,), "gate")
         pg = _address(gate, _FP32, here, "gate")
+    if max(B, N, No, Ny, D) > _MOST_INT:
+        raise SsamError(name, EUNSUPPORTED)
     branch = (po, *_token_map(src, B, N, here, "src"), *_norm(post, D, here, "post"), pg, each)
-    return here, B, N, No, D, branch, _norm(pre, D, here, "pre"), _token_map(dst, B, N, here, "dst")
+    return here, B, N, No, Ny, D, branch, _norm(pre, D, here, "pre"), _token_map(dst, B, N, here, "dst")
 
 
 def _stream_out(x, o, x_out):
@@ -871,14 +883,10 @@ def ssam_residual_norm(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre
     """x [B,N,D], o [B,No,D] bf16; src, dst int32 [N] or [B,N] (None: the tokens' own order); post, pre: (gain, shift) fp32 [D] of the LayerNorms behind the branch and
     in front of the next half, or None; gate fp32 [D] or [B,D] or None -> (x_out [B,N,D], y [B,Ny,D] bf16 or None).
     x_out may be x; y: rows that dst does not name are left as they are (None: a new one, zeros there)."""
-    here, B, N, No, D, branch, norm, to = _step_arguments(x, o, src, post, gate, dst, pre)
+    here, B, N, No, Ny, D, branch, norm, to = _step_arguments("ssam_residual_norm", x, o, src, post, gate, dst, pre, 0 if pre is None else Ny if y is None else y.shape[1])
     px, x_out = _address(x, _BF16, here, "x"), _stream_out(x, o, x_out)
-    if pre is None:
-        Ny = 0
-    else:
-        Ny = y.shape[1] if y is not None else N if Ny is None else Ny
-        if y is None:
-            y = x.new_empty((B, Ny, D)) if dst is None else x.new_zeros((B, Ny, D))
+    if y is None and pre is not None:
+        y = x.new_empty((B, Ny, D)) if dst is None else x.new_zeros((B, Ny, D))
     _shape(y, (B, Ny, D), "y")
     _check("ssam_residual_norm", lib().ssam_residual_norm(
         px, _address(x_out, _BF16, here, "x_out"), *branch, alpha, *norm, *to, eps, _address(y, _BF16, here, "y"), B, N, No, Ny, D, _raw_stream(here)))
@@ -888,9 +896,9 @@ def ssam_residual_norm(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre
 def ssam_residual_norm_i8(x, o=None, src=None, post=None, gate=None, alpha=1.0, pre=None, dst=None, eps=1e-6, Ny=None, x_out=None, codes=None, scales=None):
     """ssam_residual_norm with its rows in 8 bits -> (x_out, codes [B,Ny,D] int8, scales [B,Ny] fp32), the operand of ssam_linear_i8.
     codes, scales: rows that dst does not name are left as they are (None: new ones, zeros there)."""
-    here, B, N, No, D, branch, norm, to = _step_arguments(x, o, src, post, gate, dst, pre)
+    Ny = codes.shape[1] if codes is not None else scales.shape[1] if scales is not None else Ny
+    here, B, N, No, Ny, D, branch, norm, to = _step_arguments("ssam_residual_norm_i8", x, o, src, post, gate, dst, pre, Ny)
     px, x_out = _address(x, _BF16, here, "x"), _stream_out(x, o, x_out)
-    Ny = codes.shape[1] if codes is not None else scales.shape[1] if scales is not None else N if Ny is None else Ny
     new = x.new_empty if dst is None else x.new_zeros
     codes = new((B, Ny, D), dtype=_INT8) if codes is None else codes
     scales = new((B, Ny), dtype=_FP32) if scales is None else scales
@@ -903,6 +911,8 @@ def ssam_residual_norm_i8(x, o=None, src=None, post=None, gate=None, alpha=1.0, 
 
 
 def ssam_residual_norm_backward_workspace_bytes(B, N, D, gate_images=1) -> int:
+    if max(B, N, D, gate_images) > _MOST_INT:
+        return 0
     return lib().ssam_residual_norm_backward_workspace_bytes(B, N, D, gate_images)
 
 
@@ -911,11 +921,10 @@ def ssam_residual_norm_backward(x_out, o=None, src=None, post=None, gate=None, a
     """Gradients of ssam_residual_norm: x_out its stream, dy [B,Ny,D] and dx_out [B,N,D] (or None) bf16 the gradients of its results, the rest as given to it
     -> (dx, do, dgate, (dpost_g, dpost_b) or None, (dpre_g, dpre_b) or None).  dx may be dx_out; do: rows that src does not name are left as they are (None: a new one,
     zeros there)."""
-    here, B, N, No, D, branch, norm, to = _step_arguments(x_out, o, src, post, gate, dst, pre)
+    here, B, N, No, Ny, D, branch, norm, to = _step_arguments("ssam_residual_norm_backward", x_out, o, src, post, gate, dst, pre, 0 if dy is None else dy.shape[1])
     px = _address(x_out, _BF16, here, "x_out")
     if (pre is None) != (dy is None):
         raise ValueError("dy: the gradient of y, where there is one")
-    Ny = 0 if dy is None else dy.shape[1]
     _shape(dy, (B, Ny, D), "dy")
     dx = torch.empty_like(x_out) if dx is None else dx
     if do is None and o is not None:
