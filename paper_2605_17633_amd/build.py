@@ -53,7 +53,7 @@ def _resources(stderr: str):
 
 HOT = ("gemm_bf16_nt_", "gemm_ring_kernel", "gemm_direct_kernel", "gemm_wide_kernel", "gemm_i8_wide_", "attn_")     # kernels that are written to a register budget
 
-BACKWARD = ("backward_rows_kernel", "backward_columns_kernel", "backward_windows_kernel", "residual_norm_")                # likewise, of one wave to a SIMD with tables of 128 entries, and for rows above 1536
+BACKWARD = ("backward_rows_kernel", "backward_columns_kernel", "backward_windows_kernel", "residual_norm_")                # likewise; some have a SIMD to themselves: with tables of 128 entries, or of rows above 1536 with the second LayerNorm and the weights' gradients
 
 
 def spilled(kernels):

@@ -230,7 +230,8 @@ int by_width(int chunks, Call call)
 // Waves walk the tokens and keep their share of the sums, two vectors in registers and the others in LDS (all four in registers leave one wave to a SIMD, under whose arithmetic
 // nothing is requested); the eight waves of a workgroup add theirs up, a second launch adds the workgroups' up, a third the images', all in a fixed order: no atomics, the same bits every time.
 // Bound by HBM: 32768 x 1280 (453 MB) 87 us, 5.2 TB/s, and 4 the sums; with sums over lanes through LDS 175, without those but all sums in registers and no token requested ahead 153.
-// 784 x 768: 7.6 and 3.5 us.
+// 784 x 768: 7.6 and 3.5 us.  Rows up to 512 are bound by the instructions of a row, which are as many whatever part of its lanes it fills (16, 32 or 64): 65536 x 144 and x 256 take 41 us both (2.8 and
+// 4.9 TB/s), 65536 x 288 and x 512 66 and 74.
 struct BackArgs {
     const uint4 *x_out, *o, *dy, *dx_out;
     uint4 *dx, *d_o;
@@ -248,7 +249,9 @@ struct Sums {
     static constexpr int GH = 0, G = 1, DYH = 1 + POST, DY = 2 + POST, NV = 1 + POST + 2 * PRE, IN_REGISTERS = NV < 2 ? NV : 2, IN_LDS = NV - IN_REGISTERS;
 };
 
-// Waves of a workgroup, one to a CU.  Rows above 1536 with both norms spill 67 of the 256 registers that two waves to a SIMD have.
+// Waves of a workgroup, one to a CU.  Rows above 1536 with the second LayerNorm and the weights' gradients spill 72 of the 256 registers that two waves to a SIMD have (16384 x 2048, both norms: 125 us
+// with eight waves, 80 with four).  The other kernels of such rows fit 256, and four waves serve them as well: without the weights' gradients 63.9 us, with eight waves 65.0, without the second
+// LayerNorm 48.1 and 47.8 (16384 x 1664 0 to 6 % faster with eight, 784 x 2048 2 to 15 % slower); so the number is the width's alone.
 constexpr int back_waves(int maxc) { return maxc == 4 ? 4 : 8; }
 
 // LDS of a workgroup: both norms' factors, and the waves' sums, or room for a vector of all of them
