@@ -10,7 +10,7 @@
 //   * past the caches: C is as large as the L2s in every round, and pushed A and W out.  32768 x 3840 x 1280 as gemm_wide.h does it 192 us, with both 165 (skipping the stores: 140); one of the two alone 178.  What
 //     reads C next does not miss it: fc1, rows in 8 bits, fc2, LayerNorm of 13104 x 1280 x 5120 267 -> 237 us, of 1638 rows 52 -> 49;
 //   * tiles that are not a whole round are cut in pieces, half of them in front (192 -> 184 us before the stores were changed).
-// Measured (us; int8 library product, no scales nor bias, for comparison): 32768 x 3840 x 1280 165 (217), 13104 x 5120 x 1280 94, + GELU 114 (119), 13104 x 1280 x 5120 87 (99), + scatter-add 91, 4900 x 1280 x 1280 + scatter-add 16.1,
+// Measured (us; int8 library product, no scales nor bias, for comparison): 32768 x 3840 x 1280 160 in a loop, 173 the median of traced launches, the least of which is 165 (217), 13104 x 5120 x 1280 94, + GELU 114 (119), 13104 x 1280 x 5120 87 (99), + scatter-add 91, 4900 x 1280 x 1280 + scatter-add 16.1,
 // 4096 x 2304 x 768 12.8.  GELU costs 4.5 us a round of 256x256: its arithmetic, which nothing runs beside.  Not faster: results by whole lines of 128 bytes after an exchange between lanes (8 rows an
 // instruction, 30 % slower); two workgroups to a CU, of which one writes while the other multiplies: 128x128 in 128 registers 194 us of the first, 128x256 of four waves 187 (GELU as fast as now): they pull
 // twice and one and a half times the bytes of 256x256 from the L2.
